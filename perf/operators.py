@@ -108,7 +108,7 @@ def prepare(case, seed):
         s["type"] = _TYPES[case["out"]]
         if own:
             import paper_2605_11186_amd as cats
-            s["w"] = cats.cats_pack_matrix_int8(s["w"])   # laid out once, as the model is loaded
+            s["w"] = cats.cats_pack_quantized_matrix(s["w"])   # laid out once, as the model is loaded
             s["y"] = torch.empty(R, C, dtype=s["type"], device="cuda")
         return s
     if op == "rmsnorm":
@@ -144,17 +144,17 @@ def run(state):
         import paper_2605_11186_amd as cats
         stream = torch.cuda.current_stream()
         if op == "linear":
-            cats.cats_linear_int8(state["x"], state["x_scale"], state["w"], state["w_scale"], state["y"], stream=stream)
+            cats.cats_quantized_linear(state["x"], state["x_scale"], state["w"], state["w_scale"], state["y"], stream=stream)
             return state["y"]
         q, scale = state["q"], state["scale"]
         if op == "rmsnorm":
-            cats.cats_rmsnorm_int8(state["x"], state["gain"], EPS, q, scale, delta=state["delta"],
+            cats.cats_rmsnorm_quantize(state["x"], state["gain"], EPS, q, scale, delta=state["delta"],
                                    x_out=state.get("x_out"), stream=stream)
             return (state.get("x_out"), torch.mul(q, scale[:, None], out=state["values"]), scale)
         if op == "swiglu":
-            cats.cats_swiglu_int8(state["gate_up"], q, scale, stream=stream)
+            cats.cats_swiglu_quantize(state["gate_up"], q, scale, stream=stream)
         else:
-            cats.cats_quantize_int8(state["src"], q, scale, stream=stream)
+            cats.cats_quantize_rows(state["src"], q, scale, stream=stream)
         return (torch.mul(q, scale[:, None], out=state["values"]), scale)
     if op == "linear":
         acc = torch.matmul(state["x"].float(), state["w"].float().t())
