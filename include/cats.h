@@ -320,6 +320,62 @@ int cats_tree_attention_noalloc(const void *q, const cats_kv_layer *kv, const in
                                 int32_t n_nodes, int32_t n_heads, int32_t head_dim, int32_t max_ctx,
                                 int32_t ctx_len, void *out, void *stream);
 
+/* ---- A decoder layer in 8-bit integers (the layers of the target verification pass for a target whose
+ * weights and activations are held in 8 bits: half the bytes of the layer-weight stream).
+ *
+ * A row v of 8-bit integers carries one scale: q = v / scale rounded to whole numbers (ties to even; a quotient within
+ * 2^-15 of a tie may go either way), -127 <= q <= 127, scale = max|v| / 127 and at least 2^-126.  A row that holds an
+ * infinity or a NaN (for the norm also: whose sum of squares passes the range of float32) has q = 0 and scale = NaN; other rows do not
+ * notice.  Weights are rows in this sense, one per output column.
+ * Arithmetic before the rounding is float32, sums included.  Types of float inputs and outputs: CATS_F32, CATS_BF16.
+ * ld arguments: elements from the start of one row to the next, at least the row's length.  Rows and ld may have any
+ * alignment (that of the element type) unless said otherwise; rows whose starts are multiples of 16 bytes, with a multiple of 8 columns, are
+ * the fast case.  Bytes between a row's end and the next row are neither read nor written.
+ * Outputs must not overlap inputs or other outputs, except x_out = x.  rows = 0 enqueues nothing.  No call allocates, waits or uses
+ * scratch memory: calls on different streams may overlap, and every call can be captured into a HIP graph.  The tensors
+ * have to be usable from the current device, to which the stream belongs.
+ * CATS_EINVAL: a NULL pointer (where not optional), an unknown type, a misaligned pointer, rows < 0, a length < 1, a too small ld.
+ * CATS_ECAPACITY: rows above CATS_QUANT_MAX_ROWS, columns above CATS_QUANT_MAX_COLS (a whole row is held in
+ * registers). */
+#define CATS_F32 0
+#define CATS_BF16 1
+#define CATS_QUANT_MAX_COLS 65536
+#define CATS_QUANT_MAX_ROWS 2097152
+#define CATS_QUANT_MAX_INNER 131071 /* the product's sums, at most 2^14 * inner, fit 32 bits */
+
+/* Rows of src [rows][cols] in 8 bits: q [rows][cols], scale float32 [rows].  For activations (attention output) and, row by
+ * row, for weight matrices [out][in]. */
+int cats_quantize_rows(const void *src, int32_t src_type, int64_t src_ld, int32_t rows, int32_t cols, int8_t *q, int64_t q_ld,
+                       float *scale, void *stream);
+
+/* Residual addition, RMSNorm and rows in 8 bits: x' = x + delta, v = x' / sqrt(mean(x'^2) + eps) * gain.
+ * x: float32 [rows][cols]; delta: optional, float32 or bf16 [rows][cols]; gain: bf16 [cols]; eps > 0.
+ * x_out: float32 [rows][cols], receives x'; required with delta, NULL without; may be x (then x_out_ld = x_ld). */
+int cats_rmsnorm_quantize(const float *x, int64_t x_ld, const void *delta, int32_t delta_type, int64_t delta_ld,
+                          const void *gain, float eps, int32_t rows, int32_t cols, float *x_out, int64_t x_out_ld,
+                          int8_t *q, int64_t q_ld, float *scale, void *stream);
+
+/* SwiGLU and rows in 8 bits: gate_up [rows][2 cols] holds g | u, v = g / (1 + exp(-g)) * u. */
+int cats_swiglu_quantize(const void *gate_up, int32_t type, int64_t ld, int32_t rows, int32_t cols, int8_t *q, int64_t q_ld,
+                         float *scale, void *stream);
+
+/* One-time re-tiling of 8-bit weights W [rows][cols] (rows: output columns of the product) for cats_quantized_linear: rows are
+ * padded to a multiple of 16 and columns to a multiple of 64 with zeros; the kilobyte of row block rb and column chunk c starts at byte
+ * (rb * ceil(cols/64) + c) * 1024 and holds, for lane l < 64, the 16 values W[16 rb + l % 16][64 c + 16 (l / 16) .. +15].
+ * dst: cats_packed_quantized_bytes(rows, cols) bytes (0 for a length < 1), 16-byte aligned.  CATS_ECAPACITY: cols above
+ * CATS_QUANT_MAX_INNER. */
+size_t cats_packed_quantized_bytes(int32_t rows, int32_t cols);
+int cats_pack_quantized_matrix(const int8_t *src, int64_t src_ld, int32_t rows, int32_t cols, int8_t *dst, void *stream);
+
+/* y[t][n] = (sum over k < inner of x[t][k] W[n][k]) * x_scale[t] * w_scale[n], t < rows, n < cols: x int8 [rows][inner],
+ * 16-byte aligned, x_ld a multiple of 16 (the bytes behind a row up to the next multiple of 16 are read, but do not count);
+ * w_packed: cats_pack_quantized_matrix of W [cols][inner]; x_scale float32 [rows], w_scale float32 [cols]; y float32 or
+ * bf16.  The sums are exact; y is their product with the scales in float32, rounded once more for bf16.  All 256 values of x
+ * and W are allowed.  CATS_ECAPACITY also: inner above CATS_QUANT_MAX_INNER, cols above CATS_QUANT_MAX_ROWS,
+ * rows * cols above 2^33. */
+int cats_quantized_linear(const int8_t *x, int64_t x_ld, const float *x_scale, const int8_t *w_packed, const float *w_scale,
+                          void *y, int32_t y_type, int64_t y_ld, int32_t rows, int32_t cols, int32_t inner, void *stream);
+
 /* Measurement aid for the weight-streaming products (the layer-weight pass of the
  * "Target verification pass"; a product that rotates and appends to the cache, or applies SwiGLU,
  * is timed with that step): while enabled, every product launch made through

@@ -23,13 +23,19 @@ __all__ = ["CATS_MAX_TREE", "CATS_MAX_DEPTH", "CatsError", "ModelDesc", "LayerWe
            "cats_pack_matrix", "pack_layer", "MATRIX_FIELDS", "layer_weights_struct", "kv_array",
            "layer_array", "kv_from_rows", "kv_to_rows", "accept_result_tensor",
            "accept_result_from_tensor", "CATS_OK", "CATS_EINVAL", "CATS_ECAPACITY", "CATS_ESTATE",
-           "CATS_EHIP"]
+           "CATS_EHIP", "CATS_F32", "CATS_BF16", "CATS_QUANT_MAX_COLS", "CATS_QUANT_MAX_ROWS", "CATS_QUANT_MAX_INNER",
+           "cats_quantize_rows", "cats_rmsnorm_quantize", "cats_swiglu_quantize",
+           "cats_packed_quantized_bytes", "cats_pack_quantized_matrix", "cats_quantized_linear"]
 
 CATS_MAX_TREE = 128
 CATS_MAX_DEPTH = 16
 CATS_LOSS_MAX_K = 64
 CATS_LOSS_MAX_VOCAB = 36864
 CATS_NOALLOC_SCRATCH_BYTES = 8 << 20
+CATS_F32, CATS_BF16 = 0, 1
+CATS_QUANT_MAX_COLS = 65536
+CATS_QUANT_MAX_ROWS = 2097152
+CATS_QUANT_MAX_INNER = 131071
 CATS_OK, CATS_EINVAL, CATS_ECAPACITY, CATS_ESTATE, CATS_EHIP = 0, -1, -2, -3, -4
 
 _LIB_PATH = Path(__file__).resolve().parent / "libcats.so"
@@ -109,6 +115,15 @@ _SIGNATURES = {
                          C.c_void_p, C.c_void_p],
     "cats_tree_attention_noalloc": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                     C.c_int32, C.c_int32, C.c_void_p, C.c_void_p],
+    "cats_quantize_rows": [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p,
+                           C.c_void_p],
+    "cats_rmsnorm_quantize": [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_float, C.c_int32,
+                              C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p],
+    "cats_swiglu_quantize": [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p,
+                             C.c_void_p],
+    "cats_pack_quantized_matrix": [C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p],
+    "cats_quantized_linear": [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64,
+                              C.c_int32, C.c_int32, C.c_int32, C.c_void_p],
 }
 
 
@@ -119,7 +134,8 @@ def library_path() -> Path:
 def exported_symbols():
     """Names every build must export (those declared in include/cats.h)."""
     return sorted(list(_SIGNATURES) + ["cats_gemm_kernel_name", "cats_strerror",
-                                       "cats_layer_weight_bytes", "cats_packed_matrix_bytes"])
+                                       "cats_layer_weight_bytes", "cats_packed_matrix_bytes",
+                                       "cats_packed_quantized_bytes"])
 
 
 def library():
@@ -139,6 +155,8 @@ def library():
         lib.cats_strerror.restype = C.c_char_p
         lib.cats_packed_matrix_bytes.argtypes = [C.c_int32, C.c_int32]
         lib.cats_packed_matrix_bytes.restype = C.c_size_t
+        lib.cats_packed_quantized_bytes.argtypes = [C.c_int32, C.c_int32]
+        lib.cats_packed_quantized_bytes.restype = C.c_size_t
         lib.cats_layer_weight_bytes.argtypes = [C.c_void_p]
         lib.cats_layer_weight_bytes.restype = C.c_size_t
         lib.cats_gemm_kernel_name.argtypes = []
@@ -345,6 +363,124 @@ def cats_lm_head_argmax(ctx, hidden, g_final, w_lm, argmax_out, logits_out=None,
     """Rows are taken from hidden's shape [n_rows][hidden]."""
     _check(library().cats_lm_head_argmax(ctx, _dp(hidden), int(hidden.shape[0]), _dp(g_final), _dp(w_lm),
                                          _dp(logits_out), _dp(argmax_out), _dp(margin_out), _stream(stream)))
+
+
+def _type_code(t):
+    """CATS_F32 or CATS_BF16 of a tensor."""
+    import torch
+    code = {torch.float32: CATS_F32, torch.bfloat16: CATS_BF16}.get(t.dtype)
+    if code is None:
+        raise CatsError(CATS_EINVAL, f"float32 or bfloat16 expected, got {t.dtype}")
+    return code
+
+
+def _rows_of(name, t, dtype, rows, cols, device):
+    """Checks of a [rows][cols] operand whose rows lie in one piece each; returns its row stride in elements."""
+    if t.dtype != dtype or t.shape != (rows, cols) or t.device != device:
+        raise CatsError(CATS_EINVAL, f"{name}: {dtype} [{rows}][{cols}] on {device} expected, got {t.dtype} "
+                                     f"{list(t.shape)} on {t.device}")
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise CatsError(CATS_EINVAL, f"{name}: the elements of a row must be neighbours in memory")
+    # the stride of a single row says nothing: any that suits a row of this length will do
+    return ld if rows > 1 else max(ld, (cols + 15) // 16 * 16)
+
+
+def _vector(name, t, dtype, n, device):
+    if t.dtype != dtype or t.shape != (n,) or t.device != device or (n > 1 and t.stride(0) != 1):
+        raise CatsError(CATS_EINVAL, f"{name}: contiguous {dtype} [{n}] on {device} expected, got {t.dtype} "
+                                     f"{list(t.shape)} on {t.device}")
+
+
+def _current(device):
+    """The operators run on the current device: refuse tensors that live elsewhere."""
+    import torch
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise CatsError(CATS_EINVAL, f"tensors on {device}, which is not the current device")
+
+
+def cats_quantize_rows(src, q_out, scale_out, stream=None):
+    """Rows of src (float32 or bfloat16 [rows][cols]) as int8 with one float32 scale each."""
+    import torch
+    (rows, cols), dev = src.shape, src.device
+    code, ld = _type_code(src), _rows_of("src", src, src.dtype, rows, cols, dev)
+    q_ld = _rows_of("q_out", q_out, torch.int8, rows, cols, dev)
+    _vector("scale_out", scale_out, torch.float32, rows, dev)
+    _current(dev)
+    if rows == 0:
+        return
+    _check(library().cats_quantize_rows(src.data_ptr(), code, ld, rows, cols, q_out.data_ptr(), q_ld,
+                                        scale_out.data_ptr(), _stream(stream)))
+
+
+def cats_rmsnorm_quantize(x, gain, eps: float, q_out, scale_out, delta=None, x_out=None, stream=None):
+    """x (float32 [rows][cols]) plus delta, normalised, times gain, as int8 rows with scales.  With delta the sum
+    goes to x_out, or back to x if none is given."""
+    import torch
+    (rows, cols), dev = x.shape, x.device
+    ld = _rows_of("x", x, torch.float32, rows, cols, dev)
+    _vector("gain", gain, torch.bfloat16, cols, dev)
+    q_ld = _rows_of("q_out", q_out, torch.int8, rows, cols, dev)
+    _vector("scale_out", scale_out, torch.float32, rows, dev)
+    d_ptr, d_code, d_ld, o_ptr, o_ld = None, 0, 0, None, 0
+    if delta is not None:
+        d_ptr, d_code, d_ld = delta.data_ptr(), _type_code(delta), _rows_of("delta", delta, delta.dtype, rows, cols, dev)
+        out = x if x_out is None else x_out
+        o_ptr, o_ld = out.data_ptr(), _rows_of("x_out", out, torch.float32, rows, cols, dev)
+    elif x_out is not None:
+        raise CatsError(CATS_EINVAL, "x_out without delta: x does not change")
+    _current(dev)
+    if rows == 0:
+        return
+    _check(library().cats_rmsnorm_quantize(x.data_ptr(), ld, d_ptr, d_code, d_ld, gain.data_ptr(), eps, rows, cols, o_ptr,
+                                           o_ld, q_out.data_ptr(), q_ld, scale_out.data_ptr(), _stream(stream)))
+
+
+def cats_swiglu_quantize(gate_up, q_out, scale_out, stream=None):
+    """silu(gate) * up of gate_up (float32 or bfloat16 [rows][2 cols], gate | up) as int8 rows with scales."""
+    import torch
+    (rows, cols), dev = q_out.shape, gate_up.device
+    code, ld = _type_code(gate_up), _rows_of("gate_up", gate_up, gate_up.dtype, rows, 2 * cols, dev)
+    q_ld = _rows_of("q_out", q_out, torch.int8, rows, cols, dev)
+    _vector("scale_out", scale_out, torch.float32, rows, dev)
+    _current(dev)
+    if rows == 0:
+        return
+    _check(library().cats_swiglu_quantize(gate_up.data_ptr(), code, ld, rows, cols, q_out.data_ptr(), q_ld,
+                                          scale_out.data_ptr(), _stream(stream)))
+
+
+def cats_packed_quantized_bytes(rows: int, cols: int) -> int:
+    return int(library().cats_packed_quantized_bytes(int(rows), int(cols)))
+
+
+def cats_pack_quantized_matrix(src, stream=None):
+    """Packed copy of int8 weights [out][in] (new device tensor, int8)."""
+    import torch
+    (rows, cols), dev = src.shape, src.device
+    ld = _rows_of("src", src, torch.int8, rows, cols, dev)
+    _current(dev)
+    dst = torch.empty(cats_packed_quantized_bytes(rows, cols), dtype=torch.int8, device=dev)
+    _check(library().cats_pack_quantized_matrix(src.data_ptr(), ld, rows, cols, dst.data_ptr(), _stream(stream)))
+    return dst
+
+
+def cats_quantized_linear(x, x_scale, w_packed, w_scale, out, stream=None):
+    """out [rows][cols] (float32 or bfloat16) = (x . W) * x_scale * w_scale for int8 x [rows][inner] and packed int8 W [cols][inner]."""
+    import torch
+    (rows, inner), (_, cols), dev = x.shape, out.shape, x.device
+    code, ld = _type_code(out), _rows_of("x", x, torch.int8, rows, inner, dev)
+    y_ld = _rows_of("out", out, out.dtype, rows, cols, dev)
+    _vector("x_scale", x_scale, torch.float32, rows, dev)
+    _vector("w_scale", w_scale, torch.float32, cols, dev)
+    if inner % 16 and x.untyped_storage().nbytes() < x.storage_offset() + (rows - 1) * ld + (inner + 15) // 16 * 16:
+        raise CatsError(CATS_EINVAL, "x: its last row must be readable up to a multiple of 16 bytes")
+    _vector("w_packed", w_packed, torch.int8, (cols + 15) // 16 * ((inner + 63) // 64) * 1024, dev)
+    _current(dev)
+    if rows == 0:
+        return
+    _check(library().cats_quantized_linear(x.data_ptr(), ld, x_scale.data_ptr(), w_packed.data_ptr(), w_scale.data_ptr(),
+                                           out.data_ptr(), code, y_ld, rows, cols, inner, _stream(stream)))
 
 
 def cats_profile_gemm(ctx, enable: bool):

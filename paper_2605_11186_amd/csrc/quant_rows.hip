@@ -1,0 +1,367 @@
+// Rows in 8-bit integers with one scale each, and the steps of a decoder layer that end in such rows:
+//   q = rint(127 v / max|v|) (ties to even),  scale = max|v| / 127 (at least 2^-126)
+// for v = a source row, v = rmsnorm(x + delta) * gain, or v = silu(gate) * up.
+//
+// One pass: a row is read once, held in the registers of the threads that share it (8 values a thread and piece)
+// until its maximum is known, and written as bytes.  The kernel is bound by memory; there is no matrix work.
+#include <atomic>
+
+#include "quant.hpp"
+
+namespace {
+
+constexpr float SCALE_MIN = 0x1p-126f;   // smallest normal number: 1 / scale stays finite
+
+// Largest of a wave's unsigned values, in all lanes (see sum_lanes for the moves).
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_moved_u(uint32_t x) {
+    return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ uint32_t wave_max64(uint32_t v) {
+    const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max(p[0], p[1]);
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(r[0], r[1]);
+    v = max(v, dpp_moved_u<0x128>(v));
+    v = max(v, dpp_moved_u<0x124>(v));
+    v = max(v, dpp_moved_u<0x4E>(v));
+    return max(v, dpp_moved_u<0xB1>(v));
+}
+
+// Eight values as they lie in memory: whole pieces of 16 bytes (VEC) or one by one.
+template <class T, bool VEC>
+struct Raw;
+template <>
+struct Raw<float, true> {
+    f32x4 v[2];
+    __device__ __forceinline__ float get(int e) const { return v[e >> 2][e & 3]; }
+};
+template <>
+struct Raw<bf16_t, true> {
+    u32x4 v;
+    __device__ __forceinline__ float get(int e) const {
+        return __uint_as_float(e & 1 ? v[e >> 1] & 0xFFFF0000u : v[e >> 1] << 16);
+    }
+};
+template <>
+struct Raw<float, false> {
+    float v[8];
+    __device__ __forceinline__ float get(int e) const { return v[e]; }
+};
+template <>
+struct Raw<bf16_t, false> {
+    bf16_t v[8];
+    __device__ __forceinline__ float get(int e) const { return bf2f(v[e]); }
+};
+
+// Places of a thread's values: piece j, value e.  VEC: eight neighbours; else neighbouring threads hold neighbouring
+// values, so that a wave's load of one value each is still one run of memory.
+template <int TPR, bool VEC>
+__device__ __forceinline__ int place(int tid, int j, int e) {
+    return VEC ? (j * TPR + tid) * 8 + e : (j * 8 + e) * TPR + tid;
+}
+// Places behind the row read its last values instead (nothing counts of them): the loads need no branch.
+template <class T, int TPR, bool VEC>
+__device__ __forceinline__ Raw<T, VEC> load8(const T* row, int tid, int j, int cols) {
+    Raw<T, VEC> r;
+    if constexpr (VEC) {
+        const T* p = row + min(place<TPR, VEC>(tid, j, 0), cols - 8);
+        if constexpr (sizeof(T) == 4) {
+            r.v[0] = *reinterpret_cast<const f32x4*>(p);
+            r.v[1] = *reinterpret_cast<const f32x4*>(p + 4);
+        } else {
+            r.v = *reinterpret_cast<const u32x4*>(p);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.v[e] = row[min(place<TPR, VEC>(tid, j, e), cols - 1)];
+    }
+    return r;
+}
+
+// TPR threads share a row (64: four rows a workgroup), NC pieces of 8 values each.  T: type of the source.
+// D: type of delta (void: none).
+template <int KIND, class T, class D, int TPR, int NC, bool VEC>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kernel(QuantRowsArgs a) {
+    constexpr int ROWS_WG = TPR < 256 ? 256 / TPR : 1;
+    constexpr int WAVES = TPR / 64;
+    constexpr bool HAS_DELTA = sizeof(D) < 8;
+    const int tid = threadIdx.x % TPR;
+    const int t = blockIdx.x * ROWS_WG + threadIdx.x / TPR;
+    if (t >= a.rows) return;   // whole waves, and no barrier where a workgroup has several rows
+    const int cols = a.cols;
+    const T* src = static_cast<const T*>(a.src) + t * a.src_ld;
+
+    Raw<T, VEC> r0[NC];
+    float v[NC][8];
+    bool in[NC][VEC ? 1 : 8];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+        r0[j] = load8<T, TPR, VEC>(src, tid, j, cols);
+#pragma unroll
+        for (int e = 0; e < (VEC ? 1 : 8); ++e) in[j][e] = place<TPR, VEC>(tid, j, e) < cols;
+    }
+    if constexpr (KIND == ROWS_PLAIN) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[j][e] = in[j][VEC ? 0 : e] ? r0[j].get(e) : 0.f;
+    } else if constexpr (KIND == ROWS_SWIGLU) {
+        Raw<T, VEC> r1[NC];
+#pragma unroll
+        for (int j = 0; j < NC; ++j) r1[j] = load8<T, TPR, VEC>(src + cols, tid, j, cols);
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float g = r0[j].get(e);
+                const float h = g / (1.f + __expf(-g)) * r1[j].get(e);
+                v[j][e] = in[j][VEC ? 0 : e] ? h : 0.f;
+            }
+    } else {
+        Raw<bf16_t, VEC> rg[NC];
+        float ss = 0.f;
+        if constexpr (HAS_DELTA) {
+            Raw<D, VEC> r1[NC];
+            const D* delta = static_cast<const D*>(a.delta) + t * a.delta_ld;
+            float* out = a.x_out + t * a.x_out_ld;
+#pragma unroll
+            for (int j = 0; j < NC; ++j) r1[j] = load8<D, TPR, VEC>(delta, tid, j, cols);
+#pragma unroll
+            for (int j = 0; j < NC; ++j) rg[j] = load8<bf16_t, TPR, VEC>(a.gain, tid, j, cols);
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[j][e] = in[j][VEC ? 0 : e] ? r0[j].get(e) + r1[j].get(e) : 0.f;
+                if constexpr (VEC) {
+                    if (in[j][0]) {
+                        f32x4* p = reinterpret_cast<f32x4*>(out + place<TPR, VEC>(tid, j, 0));
+                        p[0] = f32x4{v[j][0], v[j][1], v[j][2], v[j][3]};
+                        p[1] = f32x4{v[j][4], v[j][5], v[j][6], v[j][7]};
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (in[j][e]) out[place<TPR, VEC>(tid, j, e)] = v[j][e];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+                rg[j] = load8<bf16_t, TPR, VEC>(a.gain, tid, j, cols);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[j][e] = in[j][VEC ? 0 : e] ? r0[j].get(e) : 0.f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss = fmaf(v[j][e], v[j][e], ss);
+        ss = wave_sum64(ss);
+        if constexpr (WAVES > 1) {
+            __shared__ float s_sum[WAVES];
+            if ((tid & 63) == 0) s_sum[tid >> 6] = ss;
+            __syncthreads();
+            ss = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) ss += s_sum[w];
+        }
+        // a sum of squares beyond float32 makes the row not a number, as an infinity in it does
+        const float r = ss < INFINITY ? 1.f / sqrtf(ss / static_cast<float>(cols) + a.eps) : NAN;
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[j][e] = in[j][VEC ? 0 : e] ? v[j][e] * r * rg[j].get(e) : 0.f;
+    }
+
+    // the largest |v|, as bits: ordered like the numbers, infinity above them and NaN above infinity
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[j][e]) & 0x7FFFFFFFu);
+    top = wave_max64(top);
+    if constexpr (WAVES > 1) {
+        __shared__ uint32_t s_top[WAVES];
+        if ((tid & 63) == 0) s_top[tid >> 6] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = max(top, s_top[w]);
+    }
+    const bool finite = top < 0x7F800000u;
+    const float most = fmaxf(__uint_as_float(top), 127.f * SCALE_MIN);
+    if (tid == 0) a.scale[t] = finite ? most / 127.f : NAN;
+    const float inv = 127.f / most;
+    // v * inv + 1.5 * 2^23: the sum's last bits are the nearest whole number in two's complement (one rounding, ties to even)
+    int8_t* q = a.q + t * a.q_ld;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+        uint32_t b[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = finite ? __float_as_uint(fmaf(v[j][e], inv, 12582912.f)) & 0xFFu : 0u;
+        if constexpr (VEC) {
+            if (in[j][0])
+                *reinterpret_cast<uint2*>(q + place<TPR, VEC>(tid, j, 0)) =
+                    make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (in[j][e]) q[place<TPR, VEC>(tid, j, e)] = static_cast<int8_t>(b[e]);
+        }
+    }
+}
+
+template <int KIND, class T, class D, int TPR, int NC, bool VEC>
+void launch(const QuantRowsArgs& a, hipStream_t st) {
+    constexpr int ROWS_WG = TPR < 256 ? 256 / TPR : 1;
+    hipLaunchKernelGGL((cats_quantize_rows_kernel<KIND, T, D, TPR, NC, VEC>), dim3((a.rows + ROWS_WG - 1) / ROWS_WG),
+                       dim3(TPR < 256 ? 256 : TPR), 0, st, a);
+}
+
+template <int KIND, class T, class D, bool VEC>
+void by_size(const QuantRowsArgs& a, int n_cus, hipStream_t st) {
+    const int pieces = (a.cols + 7) / 8;   // of 8 values
+    if (pieces <= 64) return launch<KIND, T, D, 64, 1, VEC>(a, st);
+    if (pieces <= 256) return launch<KIND, T, D, 256, 1, VEC>(a, st);
+    if (pieces <= 1024 && a.rows > n_cus) {
+        if (pieces <= 512) return launch<KIND, T, D, 256, 2, VEC>(a, st);
+        return launch<KIND, T, D, 256, 4, VEC>(a, st);
+    }
+    if (pieces <= 1024) return launch<KIND, T, D, 1024, 1, VEC>(a, st);
+    if (pieces <= 2048) return launch<KIND, T, D, 1024, 2, VEC>(a, st);
+    return launch<KIND, T, D, 1024, 8, VEC>(a, st);
+}
+static_assert(CATS_QUANT_MAX_ROWS <= (1 << 21), "threads of a launch: fewer than 2^32");
+static_assert(CATS_QUANT_MAX_COLS == 1024 * 8 * 8, "the longest row fills the largest workgroup's registers");
+
+// Whole pieces of 8 values: no row starts or ends inside one, and rows stay aligned.
+bool whole(const void* p, int64_t ld, size_t size) {
+    const size_t piece = size == 4 ? 16 : 8 * size;   // float32 pieces are two loads of 16 bytes
+    return (reinterpret_cast<uintptr_t>(p) | static_cast<uint64_t>(ld) * size) % piece == 0;
+}
+
+template <int KIND, class T, class D>
+void by_alignment(const QuantRowsArgs& a, int n_cus, hipStream_t st) {
+    bool vec = a.cols % 8 == 0 && whole(a.src, a.src_ld, sizeof(T)) && whole(a.q, a.q_ld, 1);
+    if (KIND == ROWS_NORM) vec = vec && whole(a.gain, 0, 2);
+    if (KIND == ROWS_NORM && sizeof(D) < 8)
+        vec = vec && whole(a.delta, a.delta_ld, sizeof(D)) && whole(a.x_out, a.x_out_ld, 4);
+    if (vec)
+        by_size<KIND, T, D, true>(a, n_cus, st);
+    else
+        by_size<KIND, T, D, false>(a, n_cus, st);
+}
+
+typedef double none_t;   // no delta
+
+bool type_ok(int32_t t) { return t == CATS_F32 || t == CATS_BF16; }
+bool aligned(const void* p, int32_t type) { return reinterpret_cast<uintptr_t>(p) % (type == CATS_F32 ? 4 : 2) == 0; }
+
+// The checks that every entry point with quantised rows shares.
+int check_rows(int32_t rows, int32_t cols, const int8_t* q, int64_t q_ld, const float* scale) {
+    if (!q || !scale || rows < 0 || cols < 1 || q_ld < cols || !aligned(scale, CATS_F32)) return CATS_EINVAL;
+    return cols > CATS_QUANT_MAX_COLS || rows > CATS_QUANT_MAX_ROWS ? CATS_ECAPACITY : CATS_OK;
+}
+int enqueue(const QuantRowsArgs& a, int kind, void* stream) {
+    if (a.rows == 0) return CATS_OK;
+    const int n_cus = quant_cus();
+    if (!n_cus) return CATS_EHIP;
+    launch_quant_rows(a, kind, n_cus, static_cast<hipStream_t>(stream));
+    return hipGetLastError() == hipSuccess ? CATS_OK : CATS_EHIP;
+}
+
+}  // namespace
+
+int quant_cus() {
+    constexpr int MAX_DEVICES = 64;
+    static std::atomic<int> known[MAX_DEVICES];   // zero: not asked yet
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) return 0;
+    n = known[dev].load(std::memory_order_relaxed);
+    if (n) return n;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return 0;
+    known[dev].store(n, std::memory_order_relaxed);
+    return n;
+}
+
+void launch_quant_rows(const QuantRowsArgs& a, int kind, int n_cus, hipStream_t st) {
+    if (a.rows < 1) return;
+    const bool f32 = a.src_type == CATS_F32;
+    if (kind == ROWS_PLAIN)
+        return f32 ? by_alignment<ROWS_PLAIN, float, none_t>(a, n_cus, st) : by_alignment<ROWS_PLAIN, bf16_t, none_t>(a, n_cus, st);
+    if (kind == ROWS_SWIGLU)
+        return f32 ? by_alignment<ROWS_SWIGLU, float, none_t>(a, n_cus, st) : by_alignment<ROWS_SWIGLU, bf16_t, none_t>(a, n_cus, st);
+    if (!a.delta) return by_alignment<ROWS_NORM, float, none_t>(a, n_cus, st);
+    return a.delta_type == CATS_F32 ? by_alignment<ROWS_NORM, float, float>(a, n_cus, st)
+                                    : by_alignment<ROWS_NORM, float, bf16_t>(a, n_cus, st);
+}
+
+extern "C" {
+
+int cats_quantize_rows(const void* src, int32_t src_type, int64_t src_ld, int32_t rows, int32_t cols, int8_t* q,
+                       int64_t q_ld, float* scale, void* stream) {
+    if (!src || !type_ok(src_type) || !aligned(src, src_type)) return CATS_EINVAL;
+    const int rc = check_rows(rows, cols, q, q_ld, scale);
+    if (rc != CATS_OK) return rc;
+    if (src_ld < cols) return CATS_EINVAL;
+    QuantRowsArgs a{};
+    a.src = src;
+    a.src_type = src_type;
+    a.src_ld = src_ld;
+    a.rows = rows;
+    a.cols = cols;
+    a.q = q;
+    a.q_ld = q_ld;
+    a.scale = scale;
+    return enqueue(a, ROWS_PLAIN, stream);
+}
+
+int cats_rmsnorm_quantize(const float* x, int64_t x_ld, const void* delta, int32_t delta_type, int64_t delta_ld,
+                          const void* gain, float eps, int32_t rows, int32_t cols, float* x_out, int64_t x_out_ld,
+                          int8_t* q, int64_t q_ld, float* scale, void* stream) {
+    if (!x || !gain || !aligned(x, CATS_F32) || !aligned(gain, CATS_BF16) || !(eps > 0.f && eps < INFINITY)) return CATS_EINVAL;
+    if ((delta == nullptr) != (x_out == nullptr)) return CATS_EINVAL;
+    const int rc = check_rows(rows, cols, q, q_ld, scale);
+    if (rc != CATS_OK) return rc;
+    if (x_ld < cols) return CATS_EINVAL;
+    if (delta && (!type_ok(delta_type) || !aligned(delta, delta_type) || !aligned(x_out, CATS_F32) || delta_ld < cols ||
+                  x_out_ld < cols || (x_out == x && x_out_ld != x_ld)))
+        return CATS_EINVAL;
+    QuantRowsArgs a{};
+    a.src = x;
+    a.src_type = CATS_F32;
+    a.src_ld = x_ld;
+    a.delta = delta;
+    a.delta_type = delta_type;
+    a.delta_ld = delta_ld;
+    a.gain = static_cast<const bf16_t*>(gain);
+    a.eps = eps;
+    a.rows = rows;
+    a.cols = cols;
+    a.x_out = x_out;
+    a.x_out_ld = x_out_ld;
+    a.q = q;
+    a.q_ld = q_ld;
+    a.scale = scale;
+    return enqueue(a, ROWS_NORM, stream);
+}
+
+int cats_swiglu_quantize(const void* gate_up, int32_t type, int64_t ld, int32_t rows, int32_t cols, int8_t* q,
+                         int64_t q_ld, float* scale, void* stream) {
+    if (!gate_up || !type_ok(type) || !aligned(gate_up, type)) return CATS_EINVAL;
+    const int rc = check_rows(rows, cols, q, q_ld, scale);
+    if (rc != CATS_OK) return rc;
+    if (ld < 2 * static_cast<int64_t>(cols)) return CATS_EINVAL;
+    QuantRowsArgs a{};
+    a.src = gate_up;
+    a.src_type = type;
+    a.src_ld = ld;
+    a.rows = rows;
+    a.cols = cols;
+    a.q = q;
+    a.q_ld = q_ld;
+    a.scale = scale;
+    return enqueue(a, ROWS_SWIGLU, stream);
+}
+
+}  // extern "C"
