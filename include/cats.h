@@ -360,8 +360,8 @@ int cats_swiglu_quantize(const void *gate_up, int32_t type, int64_t ld, int32_t 
                          float *scale, void *stream);
 
 /* One-time re-tiling of 8-bit weights W [rows][cols] (rows: output columns of the product) for cats_quantized_linear: rows are
- * padded to a multiple of 16 and columns to a multiple of 64 with zeros; the kilobyte of row block rb and column chunk c starts at byte
- * (rb * ceil(cols/64) + c) * 1024 and holds, for lane l < 64, the 16 values W[16 rb + l % 16][64 c + 16 (l / 16) .. +15].
+ * padded to a multiple of 16 and columns to a multiple of 256 with zeros; the kilobyte of row block rb and column chunk c (64
+ * columns) starts at byte (rb * 4 ceil(cols/256) + c) * 1024 and holds, for lane l < 64, the 16 values W[16 rb + l % 16][64 c + 16 (l / 16) .. +15].
  * dst: cats_packed_quantized_bytes(rows, cols) bytes (0 for a length < 1), 16-byte aligned.  CATS_ECAPACITY: cols above
  * CATS_QUANT_MAX_INNER. */
 size_t cats_packed_quantized_bytes(int32_t rows, int32_t cols);

@@ -475,7 +475,7 @@ def cats_quantized_linear(x, x_scale, w_packed, w_scale, out, stream=None):
     _vector("w_scale", w_scale, torch.float32, cols, dev)
     if inner % 16 and x.untyped_storage().nbytes() < x.storage_offset() + (rows - 1) * ld + (inner + 15) // 16 * 16:
         raise CatsError(CATS_EINVAL, "x: its last row must be readable up to a multiple of 16 bytes")
-    _vector("w_packed", w_packed, torch.int8, (cols + 15) // 16 * ((inner + 63) // 64) * 1024, dev)
+    _vector("w_packed", w_packed, torch.int8, (cols + 15) // 16 * ((inner + 255) // 256) * 4096, dev)
     _current(dev)
     if rows == 0:
         return

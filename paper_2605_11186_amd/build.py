@@ -11,7 +11,7 @@ PKG = Path(__file__).resolve().parent
 ROOT = PKG.parent
 LIB = PKG / "libcats.so"
 SOURCES = ["fused_swiglu.hip", "fused_qkv.hip", "gemm.hip", "gemv.hip", "rowops.hip", "attention.hip", "accept.hip", "loss.hip",
-           "quant_rows.hip", "quant_linear.hip", "api.hip"]
+           "quant_rows.hip", "quant_linear.hip", "quant_tiles.hip", "api.hip"]
 
 
 def _run(cmd: list[str]) -> str:

@@ -24,10 +24,11 @@ struct QuantRowsArgs {
 void launch_quant_rows(const QuantRowsArgs& a, int kind, int n_cus, hipStream_t st);
 
 // ---------------------------------------------------------------- product
-// Packed 8-bit weights: rows in blocks of 16 and columns in chunks of 64, both filled up with zeros; the kilobyte
-// of block rb and chunk c starts at (rb * chunks + c) * 1024 and holds, for lane l < 64, the 16 values
+// Packed 8-bit weights: rows in blocks of 16 and columns in chunks of 64, a multiple of four of them, filled up with zeros; the
+// kilobyte of block rb and chunk c starts at (rb * chunks + c) * 1024 and holds, for lane l < 64, the 16 values
 // W[16 rb + l % 16][64 c + 16 (l / 16) .. + 15]: a wave's operand of the 16x16x64 matrix instruction in one load.
 constexpr int QPACK_ROWS = 16, QPACK_COLS = 64, QPACK_FRAG = QPACK_ROWS * QPACK_COLS;
+inline int qpack_chunks(int cols) { return static_cast<int>((static_cast<int64_t>(cols) + 255) / 256 * 4); }
 struct QuantLinearArgs {
     const int8_t* x;       // [rows][x_ld]
     const float* x_scale;  // [rows]
@@ -36,10 +37,56 @@ struct QuantLinearArgs {
     void* y;               // [rows][y_ld], float32 or bf16
     int64_t x_ld, y_ld;
     int rows, cols, inner;
-    int chunks;            // inner in chunks of 64
+    int chunks;            // packed chunks of 64 along inner, a multiple of four
     int y_type;
 };
 void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st);
+void launch_quant_linear_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st);
+
+// y from a wave's sums: acc[i][j] holds columns n0 + 16 j .. + 3 of row t0 + 16 i.  Four columns are one store where rows
+// of y keep its alignment.
+template <int MB, int NB>
+__device__ __forceinline__ void quant_store_tile(const QuantLinearArgs& a, int t0, int n0, const i32x4 (&acc)[MB][NB]) {
+    f32x4 sw[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sw[j][e] = a.w_scale[min(n0 + 16 * j + e, a.cols - 1)];
+    float sx[MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) sx[i] = a.x_scale[min(t0 + 16 * i, a.rows - 1)];
+    const int size = a.y_type == CATS_F32 ? 4 : 2;
+    const bool whole = ((reinterpret_cast<uintptr_t>(a.y) | static_cast<uint64_t>(a.y_ld) * size) & (4 * size - 1)) == 0;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+        const int t = t0 + 16 * i;
+        if (t >= a.rows) return;
+        char* row = static_cast<char*>(a.y) + (t * a.y_ld + n0) * size;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int n = n0 + 16 * j;
+            const i32x4 v = acc[i][j];
+            const f32x4 y = f32x4{static_cast<float>(v[0]), static_cast<float>(v[1]), static_cast<float>(v[2]), static_cast<float>(v[3])} * sx[i] * sw[j];
+            const uint2 b = make_uint2(pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3]));
+            char* p = row + 16 * j * size;
+            if (whole && n + 4 <= a.cols) {
+                if (size == 4)
+                    *reinterpret_cast<f32x4*>(p) = y;
+                else
+                    *reinterpret_cast<uint2*>(p) = b;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (n + e >= a.cols) break;
+                    if (size == 4)
+                        reinterpret_cast<float*>(p)[e] = y[e];
+                    else
+                        reinterpret_cast<bf16_t*>(p)[e] = static_cast<bf16_t>((e & 2 ? b.y : b.x) >> 16 * (e & 1));
+                }
+            }
+        }
+    }
+}
 
 // Compute units of the current device (0: it could not be asked).
 int quant_cus();

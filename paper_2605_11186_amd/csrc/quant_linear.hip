@@ -12,26 +12,6 @@ namespace {
 // operands; register r of lane l of the result is D[row 4 (l / 16) + r of the first][row l % 16 of the second].  The
 // weights are the first operand: a lane's four results are neighbouring columns of y.
 
-__device__ __forceinline__ void store4(const QuantLinearArgs& a, int t, int n, i32x4 acc) {
-    if (t >= a.rows || n >= a.cols) return;
-    const float sx = a.x_scale[t];
-    float y[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = static_cast<float>(acc[e]) * sx * a.w_scale[min(n + e, a.cols - 1)];
-    const int64_t at = t * a.y_ld + n;
-    if (a.y_type == CATS_F32) {
-        float* p = static_cast<float*>(a.y) + at;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (n + e < a.cols) p[e] = y[e];
-    } else {
-        bf16_t* p = static_cast<bf16_t*>(a.y) + at;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (n + e < a.cols) p[e] = f2bf(y[e]);
-    }
-}
-
 // A workgroup owns a tile of 16 MB rows and 16 NB columns; its waves split the chunks of k among them and add up their
 // sums through LDS.
 template <int MB, int NB, int WAVES>
@@ -75,7 +55,8 @@ __global__ __launch_bounds__(64 * WAVES) void cats_quant_linear_rows(QuantLinear
         i32x4 sum = s_acc[0][f][lane];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) sum += s_acc[w][f][lane];
-        store4(a, (mt * MB + f / NB) * 16 + (lane & 15), (nt * NB + f % NB) * 16 + 4 * (lane >> 4), sum);
+        const i32x4 one[1][1] = {{sum}};
+        quant_store_tile<1, 1>(a, (mt * MB + f / NB) * 16 + (lane & 15), (nt * NB + f % NB) * 16 + 4 * (lane >> 4), one);
     }
 }
 
@@ -105,17 +86,19 @@ __global__ __launch_bounds__(256) void cats_quant_pack(const int8_t* src, int64_
 }
 
 int64_t frags_of(int32_t rows, int32_t cols) {
-    return (static_cast<int64_t>(rows) + QPACK_ROWS - 1) / QPACK_ROWS * ((static_cast<int64_t>(cols) + QPACK_COLS - 1) / QPACK_COLS);
+    return (static_cast<int64_t>(rows) + QPACK_ROWS - 1) / QPACK_ROWS * qpack_chunks(cols);
 }
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
 }  // namespace
 
-void launch_quant_linear(const QuantLinearArgs& a, int, hipStream_t st) {
+void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
     if (a.rows < 1) return;
     if (a.rows <= 16)
         launch_rows<1, 1, 8>(a, st);
+    else if (a.rows >= 256 && a.x_ld < (1 << 23))
+        launch_quant_linear_tiles(a, n_cus, st);
     else
         launch_rows<4, 2, 4>(a, st);
 }
@@ -131,7 +114,7 @@ int cats_pack_quantized_matrix(const int8_t* src, int64_t src_ld, int32_t rows, 
     if (cols > CATS_QUANT_MAX_INNER || rows > CATS_QUANT_MAX_ROWS) return CATS_ECAPACITY;
     const int64_t frags = frags_of(rows, cols);
     hipLaunchKernelGGL(cats_quant_pack, dim3(static_cast<unsigned>(std::min<int64_t>((frags + 3) / 4, 1 << 16))), dim3(256), 0, static_cast<hipStream_t>(stream),
-                       src, src_ld, dst, rows, cols, (cols + QPACK_COLS - 1) / QPACK_COLS, frags);
+                       src, src_ld, dst, rows, cols, qpack_chunks(cols), frags);
     return hipGetLastError() == hipSuccess ? CATS_OK : CATS_EHIP;
 }
 
@@ -161,7 +144,7 @@ int cats_quantized_linear(const int8_t* x, int64_t x_ld, const float* x_scale, c
     a.rows = rows;
     a.cols = cols;
     a.inner = inner;
-    a.chunks = (inner + QPACK_COLS - 1) / QPACK_COLS;
+    a.chunks = qpack_chunks(inner);
     launch_quant_linear(a, n_cus, static_cast<hipStream_t>(stream));
     return hipGetLastError() == hipSuccess ? CATS_OK : CATS_EHIP;
 }

@@ -1,0 +1,141 @@
+// The product of 8-bit integers for many rows (prompts): bound by the matrix instructions.
+#include <algorithm>
+#include <type_traits>
+
+#include "quant.hpp"
+
+namespace {
+
+// 64 lanes copy 16 bytes each from base + their own offset to 1024 consecutive bytes of LDS (at byte `lds`), with no
+// register between.  Counted in vmcnt like a load; the compiler does not see it and waits for nothing on its account.
+__device__ __forceinline__ void copy_to_lds(const int8_t* base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+
+// A workgroup of WM x WN waves owns a tile of BM = 16 WM MB rows of X and BN = 16 WN NB columns, a wave MB x NB blocks of
+// 16 x 16.  X passes through LDS in steps of 128 values of k, NS - 1 steps ahead; W's packed fragments go straight from
+// memory into the registers of the matrix instruction.
+template <int WM, int WN, int MB, int NB, int NS, int WS>
+__global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLinearArgs a, int m_tiles, int n_tiles) {
+    constexpr int WAVES = WM * WN, BM = 16 * WM * MB, BN = 16 * WN * NB;
+    constexpr int COPIES = BM / 8 / WAVES;   // of a wave and step: 8 rows of 128 bytes each
+    static_assert(4 % WS == 0, "places of W come round again after a pair of steps");
+    static_assert(COPIES * 8 * WAVES == BM, "rows dealt evenly");
+    __shared__ __align__(1024) int8_t s_x[NS][BM * 128];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+
+    // workgroup b runs on XCD b % 8: an XCD takes a run of tiles, in bands of 8 row tiles
+    const int total = m_tiles * n_tiles, xcd = blockIdx.x & 7, per = total >> 3, rem = total & 7;
+    const int id = xcd * per + min(xcd, rem) + (blockIdx.x >> 3);
+    constexpr int BAND = 4;
+    const int band = id / (BAND * n_tiles), in_band = id - band * BAND * n_tiles;
+    const int band_rows = min(BAND, m_tiles - band * BAND);
+    const int mt = __builtin_amdgcn_readfirstlane(band * BAND + in_band % band_rows), nt = __builtin_amdgcn_readfirstlane(in_band / band_rows);
+
+    const int steps = a.chunks >> 1;
+    const int k_last = (a.inner - 1) / 16 * 16;
+    const int n_rb = (a.cols + QPACK_ROWS - 1) / QPACK_ROWS;
+    // X: lane l copies piece (l % 8) ^ (l / 8) of row l / 8 of its eight rows: piece p of row r lies at place p ^ (r % 8) of
+    // the row's 128 bytes, so that the eight lanes that read neighbouring rows at once find different banks
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    const int8_t* x0 = a.x + static_cast<int64_t>(mt) * BM * a.x_ld;
+    uint32_t xo[COPIES];   // the launcher sees to it that a tile of X spans less than 2^31 bytes
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i)
+        xo[i] = min((wave * COPIES + i) * 8 + (lane >> 3), a.rows - 1 - mt * BM) * static_cast<int>(a.x_ld);
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&s_x[0][0])) + wave * COPIES * 1024;
+    auto copy_step = [&](int s, int slot) {
+        // past the end of a row of X the weights are zeros: any value will do there
+        const int k = min(s * 128 + piece, k_last);
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) copy_to_lds(x0, xo[i] + k, lds0 + slot * (BM * 128) + i * 1024);
+    };
+    // W
+    const int rb0 = nt * (BN / 16) + wn * NB;   // first row block of this wave; past the last one (and past the last step) zeros are read
+    const int64_t w_at = static_cast<int64_t>(rb0) * a.chunks * QPACK_FRAG;
+    const int w_bytes = __builtin_amdgcn_readfirstlane(max(min(NB, n_rb - rb0), 0) * a.chunks * QPACK_FRAG);
+    const __amdgpu_buffer_rsrc_t w_buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(a.w + w_at), 0, w_bytes, 0x00020000);
+    const int wo = lane * 16;
+    i32x4 w[WS][NB];   // chunk c in place c % WS, WS - 1 chunks ahead (WS = 2: reloaded behind its products)
+    auto load_w = [&](int c, i32x4(&to)[NB]) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            to[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_buf, wo, (j * a.chunks + c) * QPACK_FRAG, 0));
+    };
+    i32x4 acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+
+    const int r = lane & 15, g = lane >> 4;
+    const int8_t* xs = &s_x[0][0] + (wm * MB * 16 + r) * 128;
+    // fragment f of a step: block f % MB of rows, chunk f / MB
+    const int at[2] = {(g ^ (r & 7)) * 16, ((4 + g) ^ (r & 7)) * 16};
+    auto read_x = [&](int slot, int f) { return *reinterpret_cast<const i32x4*>(xs + slot * (BM * 128) + (f % MB) * 2048 + at[f / MB]); };
+    constexpr int AHEAD = 4;   // fragments of X read ahead of their products, across the steps' border
+    i32x4 x[AHEAD];
+    auto next_slot = [](int slot) { return slot == NS - 1 ? 0 : slot + 1; };
+    // u: parity of the step
+    auto step = [&](int s, int slot, auto u_) {
+        constexpr int u = decltype(u_)::value;
+        // The copies for step s + 1 are older than all that the two steps before issued; then everybody's are there, and
+        // nobody reads the slot of step s - 1 any more.
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)" ::"n"(COPIES + 2 * NB), "n"(AHEAD) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        copy_step(s + NS - 1, slot == 0 ? NS - 1 : slot - 1);   // (steps that do not exist go where nobody reads)
+        const int slot1 = next_slot(slot);
+#pragma unroll
+        for (int f = 0; f < 2 * MB; ++f) {
+            const int i = f % MB, h = f / MB;
+            if (i == 0) load_w(2 * s + h + WS - 1, w[(2 * u + h + WS - 1) % WS]);
+            const i32x4 xf = x[f % AHEAD];
+            x[f % AHEAD] = f + AHEAD < 2 * MB ? read_x(slot, f + AHEAD) : read_x(slot1, f + AHEAD - 2 * MB);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[(2 * u + h) % WS][j], xf, acc[i][j], 0, 0, 0);
+        }
+        // the order of the step: requests for W, then a fragment of X for each that is multiplied
+#pragma unroll
+        for (int f = 0; f < 2 * MB; ++f) {
+            if (f % MB == 0) __builtin_amdgcn_sched_group_barrier(0x020, NB, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s)
+        copy_step(s, s);
+#pragma unroll
+    for (int c = 0; c < WS - 1; ++c) load_w(c, w[c]);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((WS - 1) * NB) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int f = 0; f < AHEAD; ++f) x[f] = read_x(0, f);
+    int slot = 0, s = 0;
+    for (; s < steps; s += 2) {   // packed weights end with a whole pair of steps
+        step(s, slot, std::integral_constant<int, 0>{});
+        slot = next_slot(slot);
+        step(s + 1, slot, std::integral_constant<int, 1>{});
+        slot = next_slot(slot);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy may land after the workgroup's end
+    quant_store_tile<MB, NB>(a, mt * BM + wm * MB * 16 + r, nt * BN + wn * NB * 16 + 4 * g, acc);
+}
+
+template <int WM, int WN, int MB, int NB, int NS, int WS>
+void launch_tiles(const QuantLinearArgs& a, hipStream_t st) {
+    constexpr int BM = 16 * WM * MB, BN = 16 * WN * NB;
+    const int m_tiles = (a.rows + BM - 1) / BM, n_tiles = (a.cols + BN - 1) / BN;
+    hipLaunchKernelGGL((cats_quant_linear_tiles<WM, WN, MB, NB, NS, WS>), dim3(static_cast<unsigned>(m_tiles) * n_tiles),
+                       dim3(64 * WM * WN), 0, st, a, m_tiles, n_tiles);
+}
+
+}  // namespace
+
+void launch_quant_linear_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
+    (void)n_cus;
+    launch_tiles<2, 4, 8, 4, 4, 4>(a, st);
+}

@@ -279,7 +279,7 @@ def test_pack_layout():
     for rows, cols in [(16, 64), (5, 3), (33, 130), (100, 1001)]:
         w = whole_numbers(rng, rows, cols)
         packed = cats.cats_pack_quantized_matrix(w).cpu().numpy()
-        full = np.zeros(((rows + 15) // 16 * 16, (cols + 63) // 64 * 64), np.int8)
+        full = np.zeros(((rows + 15) // 16 * 16, (cols + 255) // 256 * 256), np.int8)
         full[:rows, :cols] = w.cpu().numpy()
         # [row block][row][chunk][quarter][16] -> [row block][chunk][quarter][row][16]
         want = full.reshape(-1, 16, full.shape[1] // 64, 4, 16).transpose(0, 2, 3, 1, 4).reshape(-1)

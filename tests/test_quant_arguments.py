@@ -70,9 +70,9 @@ def test_quantized_linear(changed, status):
 
 
 def test_packed_bytes():
-    assert cats.cats_packed_quantized_bytes(1, 1) == 1024
-    assert cats.cats_packed_quantized_bytes(16, 64) == 1024
-    assert cats.cats_packed_quantized_bytes(17, 65) == 4096
+    assert cats.cats_packed_quantized_bytes(1, 1) == 4096
+    assert cats.cats_packed_quantized_bytes(16, 256) == 4096
+    assert cats.cats_packed_quantized_bytes(17, 257) == 16384
     assert cats.cats_packed_quantized_bytes(0, 64) == cats.cats_packed_quantized_bytes(64, -1) == 0
     assert cats.cats_packed_quantized_bytes(2 ** 21, 131071) == 2 ** 21 * 131072   # beyond 32 bits
 
@@ -81,7 +81,7 @@ def test_binding_refuses_what_does_not_fit():
     """Shapes, types and places that the C call cannot see."""
     x, q, s = torch.zeros(2, 64), torch.zeros(2, 64, dtype=torch.int8), torch.zeros(2)
     g = torch.zeros(64, dtype=torch.bfloat16)
-    w, sw, y = torch.zeros(1024, dtype=torch.int8), torch.zeros(16), torch.zeros(2, 16)
+    w, sw, y = torch.zeros(4096, dtype=torch.int8), torch.zeros(16), torch.zeros(2, 16)
     bad = [
         lambda: cats.cats_quantize_rows(x.double(), q, s),
         lambda: cats.cats_quantize_rows(x, q[:, :63], s),
@@ -94,7 +94,7 @@ def test_binding_refuses_what_does_not_fit():
         lambda: cats.cats_rmsnorm_quantize(x, g, 1e-6, q, s, delta=x[:1]),
         lambda: cats.cats_swiglu_quantize(x, q, s),
         lambda: cats.cats_pack_quantized_matrix(q.float()),
-        lambda: cats.cats_quantized_linear(q, s, w[:512], sw, y),
+        lambda: cats.cats_quantized_linear(q, s, w[:1024], sw, y),
         lambda: cats.cats_quantized_linear(q, s, w, sw, y.half()),
         lambda: cats.cats_quantized_linear(q, s, w, sw[:8], y),
         lambda: cats.cats_quantized_linear(torch.zeros(1, 63, dtype=torch.int8), s[:1], w, sw, y[:1]),   # 63 bytes of memory
