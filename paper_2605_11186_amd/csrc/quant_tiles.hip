@@ -20,6 +20,7 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
     constexpr int WAVES = WM * WN, BM = 16 * WM * MB, BN = 16 * WN * NB;
     constexpr int COPIES = BM / 8 / WAVES;   // of a wave and step: 8 rows of 128 bytes each
     static_assert(4 % WS == 0, "places of W come round again after a pair of steps");
+    static_assert(MB % NB == 0 && 2 * MB % COPIES == 0, "requests dealt evenly");
     static_assert(COPIES * 8 * WAVES == BM, "rows dealt evenly");
     __shared__ __align__(1024) int8_t s_x[NS][BM * 128];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -45,23 +46,23 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
     for (int i = 0; i < COPIES; ++i)
         xo[i] = min((wave * COPIES + i) * 8 + (lane >> 3), a.rows - 1 - mt * BM) * static_cast<int>(a.x_ld);
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&s_x[0][0])) + wave * COPIES * 1024;
-    auto copy_step = [&](int s, int slot) {
+    auto copy_piece = [&](int s, int slot, int i) {
         // past the end of a row of X the weights are zeros: any value will do there
-        const int k = min(s * 128 + piece, k_last);
-#pragma unroll
-        for (int i = 0; i < COPIES; ++i) copy_to_lds(x0, xo[i] + k, lds0 + slot * (BM * 128) + i * 1024);
+        copy_to_lds(x0, xo[i] + min(s * 128 + piece, k_last), lds0 + slot * (BM * 128) + i * 1024);
     };
     // W
-    const int rb0 = nt * (BN / 16) + wn * NB;   // first row block of this wave; past the last one (and past the last step) zeros are read
-    const int64_t w_at = static_cast<int64_t>(rb0) * a.chunks * QPACK_FRAG;
-    const int w_bytes = __builtin_amdgcn_readfirstlane(max(min(NB, n_rb - rb0), 0) * a.chunks * QPACK_FRAG);
-    const __amdgpu_buffer_rsrc_t w_buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(a.w + w_at), 0, w_bytes, 0x00020000);
-    const int wo = lane * 16;
-    i32x4 w[WS][NB];   // chunk c in place c % WS, WS - 1 chunks ahead (WS = 2: reloaded behind its products)
-    auto load_w = [&](int c, i32x4(&to)[NB]) {
+    // (row blocks and chunks that do not exist are read from the last ones: their products are not stored, or not made)
+    const int rb0 = min(nt * (BN / 16) + wn * NB, n_rb - 1);
+    const int w_bytes = __builtin_amdgcn_readfirstlane(min(NB, n_rb - rb0) * a.chunks * QPACK_FRAG);
+    const __amdgpu_buffer_rsrc_t w_buf = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<int8_t*>(a.w + static_cast<int64_t>(rb0) * a.chunks * QPACK_FRAG), 0, w_bytes, 0x00020000);
+    int w_at[NB];
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
-            to[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_buf, wo, (j * a.chunks + c) * QPACK_FRAG, 0));
+    for (int j = 0; j < NB; ++j) w_at[j] = __builtin_amdgcn_readfirstlane(min(j, n_rb - 1 - rb0) * a.chunks * QPACK_FRAG);
+    const int wo = lane * 16;
+    i32x4 w[WS][NB];   // chunk c in place c % WS, WS - 1 chunks ahead
+    auto load_w = [&](int c, int j) {
+        return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_buf, wo, w_at[j] + min(c, a.chunks - 1) * QPACK_FRAG, 0));
     };
     i32x4 acc[MB][NB];
 #pragma unroll
@@ -80,35 +81,41 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
     // u: parity of the step
     auto step = [&](int s, int slot, auto u_) {
         constexpr int u = decltype(u_)::value;
-        // The copies for step s + 1 are older than all that the two steps before issued; then everybody's are there, and
-        // nobody reads the slot of step s - 1 any more.
+        // Requests are dealt out over the step, one between some products each: issued together they hold up the products behind
+        // them (49 -> 43 us for 256 x 4096 x 4096).  Copies of step s - 2 and before, that is for step s + 1, are older than
+        // all that step s - 1 issued; then everybody's are there, and nobody reads the slot of step s - 1 any
+        // more: the copies for step s + NS - 1 go there (those of
+        // steps that do not exist are read by nobody).
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)" ::"n"(COPIES + 2 * NB), "n"(AHEAD) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        copy_step(s + NS - 1, slot == 0 ? NS - 1 : slot - 1);   // (steps that do not exist go where nobody reads)
         const int slot1 = next_slot(slot);
 #pragma unroll
         for (int f = 0; f < 2 * MB; ++f) {
             const int i = f % MB, h = f / MB;
-            if (i == 0) load_w(2 * s + h + WS - 1, w[(2 * u + h + WS - 1) % WS]);
+            if (i % (MB / NB) == 0) w[(2 * u + h + WS - 1) % WS][i / (MB / NB)] = load_w(2 * s + h + WS - 1, i / (MB / NB));
+            if (f % (2 * MB / COPIES) == 1) copy_piece(s + NS - 1, slot == 0 ? NS - 1 : slot - 1, f / (2 * MB / COPIES));
             const i32x4 xf = x[f % AHEAD];
             x[f % AHEAD] = f + AHEAD < 2 * MB ? read_x(slot, f + AHEAD) : read_x(slot1, f + AHEAD - 2 * MB);
 #pragma unroll
             for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[(2 * u + h) % WS][j], xf, acc[i][j], 0, 0, 0);
         }
-        // the order of the step: requests for W, then a fragment of X for each that is multiplied
+        // the order of the step: a fragment of X for each that is multiplied, a request for W at each second
 #pragma unroll
         for (int f = 0; f < 2 * MB; ++f) {
-            if (f % MB == 0) __builtin_amdgcn_sched_group_barrier(0x020, NB, 0);
+            if (f % (MB / NB) == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
     };
 #pragma unroll
     for (int s = 0; s < NS - 1; ++s)
-        copy_step(s, s);
 #pragma unroll
-    for (int c = 0; c < WS - 1; ++c) load_w(c, w[c]);
+        for (int i = 0; i < COPIES; ++i) copy_piece(s, s, i);
+#pragma unroll
+    for (int c = 0; c < WS - 1; ++c)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) w[c][j] = load_w(c, j);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"((WS - 1) * NB) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
