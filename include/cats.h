@@ -341,6 +341,7 @@ int cats_tree_attention_noalloc(const void *q, const cats_kv_layer *kv, const in
 #define CATS_BF16 1
 #define CATS_QUANT_MAX_COLS 65536
 #define CATS_QUANT_MAX_ROWS 2097152
+#define CATS_QUANT_MAX_LD 8388608
 #define CATS_QUANT_MAX_INNER 131071 /* the product's sums, at most 2^14 * inner, fit 32 bits */
 
 /* Rows of src [rows][cols] in 8 bits: q [rows][cols], scale float32 [rows].  For activations (attention output) and, row by
@@ -372,7 +373,7 @@ int cats_pack_quantized_matrix(const int8_t *src, int64_t src_ld, int32_t rows, 
  * w_packed: cats_pack_quantized_matrix of W [cols][inner]; x_scale float32 [rows], w_scale float32 [cols]; y float32 or
  * bf16.  The sums are exact; y is their product with the scales in float32, rounded once more for bf16.  All 256 values of x
  * and W are allowed.  CATS_ECAPACITY also: inner above CATS_QUANT_MAX_INNER, cols above CATS_QUANT_MAX_ROWS,
- * rows * cols above 2^33. */
+ * x_ld not below CATS_QUANT_MAX_LD, rows * cols above 2^33. */
 int cats_quantized_linear(const int8_t *x, int64_t x_ld, const float *x_scale, const int8_t *w_packed, const float *w_scale,
                           void *y, int32_t y_type, int64_t y_ld, int32_t rows, int32_t cols, int32_t inner, void *stream);
 

@@ -23,7 +23,7 @@ __all__ = ["CATS_MAX_TREE", "CATS_MAX_DEPTH", "CatsError", "ModelDesc", "LayerWe
            "cats_pack_matrix", "pack_layer", "MATRIX_FIELDS", "layer_weights_struct", "kv_array",
            "layer_array", "kv_from_rows", "kv_to_rows", "accept_result_tensor",
            "accept_result_from_tensor", "CATS_OK", "CATS_EINVAL", "CATS_ECAPACITY", "CATS_ESTATE",
-           "CATS_EHIP", "CATS_F32", "CATS_BF16", "CATS_QUANT_MAX_COLS", "CATS_QUANT_MAX_ROWS", "CATS_QUANT_MAX_INNER",
+           "CATS_EHIP", "CATS_F32", "CATS_BF16", "CATS_QUANT_MAX_COLS", "CATS_QUANT_MAX_ROWS", "CATS_QUANT_MAX_LD", "CATS_QUANT_MAX_INNER",
            "cats_quantize_rows", "cats_rmsnorm_quantize", "cats_swiglu_quantize",
            "cats_packed_quantized_bytes", "cats_pack_quantized_matrix", "cats_quantized_linear"]
 
@@ -35,6 +35,7 @@ CATS_NOALLOC_SCRATCH_BYTES = 8 << 20
 CATS_F32, CATS_BF16 = 0, 1
 CATS_QUANT_MAX_COLS = 65536
 CATS_QUANT_MAX_ROWS = 2097152
+CATS_QUANT_MAX_LD = 8388608
 CATS_QUANT_MAX_INNER = 131071
 CATS_OK, CATS_EINVAL, CATS_ECAPACITY, CATS_ESTATE, CATS_EHIP = 0, -1, -2, -3, -4
 

@@ -1,0 +1,30 @@
+// Which tile a product of 8-bit integers is cut into.  Plain C++: the host decides, a CPU test asks it.
+#pragma once
+#include <stdint.h>
+
+// A launch takes about as long as the compute unit with the most tiles needs for their operands, rows of X and of W alike:
+// rounds of tiles times (BM + BN).  Measured at inner = 4096 and 4096 columns (us): 1.2 + 0.065 rounds (BM + BN), within
+// 10 % from 63 to 512 rows, for the tiles of up to 128 x 64; the larger ones, which the matrix instructions bind, count as
+// what they measure in this unit.  (With few rows and many columns the weights' way from memory comes on top for all alike:
+// 90 MB of weights take 15 us with one row, 20 with 63.)
+struct QuantTile {
+    int bm, bn, cost;   // rows, columns, cost of a round of one tile per compute unit
+};
+constexpr QuantTile QUANT_TILES[] = {{16, 16, 32},   {16, 32, 48},   {32, 32, 64},    {64, 32, 96},   {64, 48, 112},
+                                     {64, 64, 128},  {64, 96, 160},  {96, 96, 192},   {128, 64, 192}, {128, 96, 250},
+                                     {128, 128, 350}, {128, 256, 500}, {256, 256, 700}};
+constexpr int N_QUANT_TILES = sizeof(QUANT_TILES) / sizeof(QUANT_TILES[0]);
+inline int quant_tile_choice(int rows, int cols, int n_cus) {
+    int best = 0;
+    int64_t least = INT64_MAX;
+    for (int i = 0; i < N_QUANT_TILES; ++i) {
+        const QuantTile& c = QUANT_TILES[i];
+        const int64_t tiles = ((int64_t{rows} + c.bm - 1) / c.bm) * ((int64_t{cols} + c.bn - 1) / c.bn);
+        const int64_t cost = (tiles + n_cus - 1) / n_cus * c.cost;
+        if (cost <= least) {   // of equals the larger tile: fewer bytes
+            least = cost;
+            best = i;
+        }
+    }
+    return best;
+}

@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "quant.hpp"
+#include "quant_choice.hpp"
 
 namespace {
 
@@ -12,59 +13,112 @@ namespace {
 // operands; register r of lane l of the result is D[row 4 (l / 16) + r of the first][row l % 16 of the second].  The
 // weights are the first operand: a lane's four results are neighbouring columns of y.
 
-// A workgroup owns a tile of 16 MB rows and 16 NB columns; its waves split the chunks of k among them and add up their
-// sums through LDS.
-template <int MB, int NB, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void cats_quant_linear_rows(QuantLinearArgs a, int m_tiles) {
-    __shared__ i32x4 s_acc[WAVES][MB * NB][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int mt = blockIdx.x % m_tiles, nt = blockIdx.x / m_tiles;
+// A workgroup owns a tile of 16 MB rows and 16 NB columns; its KW waves take turns at the steps of 128 values of k and add
+// up their sums through LDS at the end.  Each wave keeps NS of its steps in a ring of LDS that nobody else touches: it waits
+// for its own copies only, reads a step's fragments, sends for the step that takes their place, and multiplies.
+template <int MB, int NB, int KW, int NS>
+__global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearArgs a, int m_tiles, int n_tiles) {
+    constexpr int COPIES = 2 * (MB + NB), STEP = COPIES * 1024;   // of a step: copies of 1 KB, bytes
+    static_assert((NS - 1) * COPIES < 64, "vmcnt");
+    constexpr int RING = KW * NS * STEP;
+    // the waves' sums meet in parts of PB row blocks that fit where the ring was
+    constexpr int PB = KW * MB * NB * 1024 <= RING ? MB : MB / 2;
+    static_assert(KW * PB * NB * 1024 <= RING && MB % PB == 0, "a part of the sums fits the ring");
+    __shared__ __align__(1024) int8_t s_lds[RING];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int mt, nt;
+    quant_tile_of(m_tiles, n_tiles, mt, nt);
     const int n_rb = (a.cols + QPACK_ROWS - 1) / QPACK_ROWS;
     const int k_last = (a.inner - 1) / 16 * 16;
-    const int8_t* xp[MB];
+    const int steps = (a.inner + 127) >> 7;   // (the packed weights may have one step of zeros more)
+    const int mine = (steps - wave + KW - 1) / KW;
+
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;   // places of X in LDS: see cats_quant_linear_tiles
+    const int8_t* x0 = a.x + static_cast<int64_t>(mt) * 16 * MB * a.x_ld;
+    uint32_t xo[2 * MB];
+#pragma unroll
+    for (int i = 0; i < 2 * MB; ++i) xo[i] = min(i * 8 + (lane >> 3), a.rows - 1 - mt * 16 * MB) * static_cast<int>(a.x_ld);
     const int8_t* wp[NB];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) xp[i] = a.x + min((mt * MB + i) * 16 + (lane & 15), a.rows - 1) * a.x_ld;
+    for (int j = 0; j < NB; ++j) wp[j] = a.w + static_cast<int64_t>(min(nt * NB + j, n_rb - 1)) * a.chunks * QPACK_FRAG;
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&s_lds[0])) + wave * NS * STEP;
+    auto fetch = [&](int i, int slot) {   // the i-th of this wave's steps
+        const int s = wave + i * KW, k = min(s * 128 + piece, k_last);
+        const uint32_t to = lds0 + slot * STEP;
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
-        wp[i] = a.w + static_cast<int64_t>(min(nt * NB + i, n_rb - 1)) * a.chunks * QPACK_FRAG + lane * 16;
+        for (int j = 0; j < NB; ++j) {
+            copy_to_lds(wp[j] + s * 2048, lane * 16, to + j * 2048);
+            copy_to_lds(wp[j] + s * 2048 + 1024, lane * 16, to + j * 2048 + 1024);
+        }
+#pragma unroll
+        for (int p = 0; p < 2 * MB; ++p) copy_to_lds(x0, xo[p] + k, to + NB * 2048 + p * 1024);
+    };
     i32x4 acc[MB][NB];
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-    for (int c = wave; c < a.chunks; c += WAVES) {
-        i32x4 x[MB], w[NB];
-        // past the end of a row of X the weights are zeros: any value will do there
-        const int k = min(c * QPACK_COLS + (lane >> 4) * 16, k_last);
+    const int r = lane & 15, g = lane >> 4;
 #pragma unroll
-        for (int i = 0; i < NB; ++i) w[i] = *reinterpret_cast<const i32x4*>(wp[i] + static_cast<int64_t>(c) * QPACK_FRAG);
+    for (int i = 0; i < NS; ++i)
+        if (i < mine) fetch(i, i);
+    int slot = 0;
+    for (int i = 0; i < mine; ++i) {
+        const int behind = mine - 1 - i;   // steps that are under way behind this one, at most NS - 1
+        if (behind >= NS - 1)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 1) * COPIES) : "memory");
+        else if (NS > 2 && behind == 2)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NS > 3 ? 2 * COPIES : 0) : "memory");
+        else if (behind == 1)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NS > 2 ? COPIES : 0) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const int8_t* from = &s_lds[0] + (wave * NS + slot) * STEP;
+        i32x4 w[2][NB], x[2][MB];
 #pragma unroll
-        for (int i = 0; i < MB; ++i) x[i] = *reinterpret_cast<const i32x4*>(xp[i] + k);
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int i = 0; i < MB; ++i)
+            for (int j = 0; j < NB; ++j) w[h][j] = *reinterpret_cast<const i32x4*>(from + j * 2048 + h * 1024 + lane * 16);
 #pragma unroll
-            for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j], x[i], acc[i][j], 0, 0, 0);
+            for (int b = 0; b < MB; ++b)
+                x[h][b] = *reinterpret_cast<const i32x4*>(from + NB * 2048 + (b * 16 + r) * 128 + ((4 * h + g) ^ (r & 7)) * 16);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the fragments are in registers: their place is free
+        if (i + NS < mine) fetch(i + NS, slot);
+        slot = slot == NS - 1 ? 0 : slot + 1;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int b = 0; b < MB; ++b)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[b][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[h][j], x[h][b], acc[b][j], 0, 0, 0);
     }
+    const int t0 = mt * 16 * MB + r, n0 = nt * 16 * NB + 4 * g;
+    {
+        i32x4* sums = reinterpret_cast<i32x4*>(&s_lds[0]);
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+        for (int b0 = 0; b0 < MB; b0 += PB) {
+            __syncthreads();   // nobody needs its ring, or the part before, any more
 #pragma unroll
-        for (int j = 0; j < NB; ++j) s_acc[wave][i * NB + j][lane] = acc[i][j];
-    __syncthreads();
-    for (int f = wave; f < MB * NB; f += WAVES) {
-        i32x4 sum = s_acc[0][f][lane];
+            for (int b = 0; b < PB; ++b)
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) sum += s_acc[w][f][lane];
-        const i32x4 one[1][1] = {{sum}};
-        quant_store_tile<1, 1>(a, (mt * MB + f / NB) * 16 + (lane & 15), (nt * NB + f % NB) * 16 + 4 * (lane >> 4), one);
+                for (int j = 0; j < NB; ++j) sums[(wave * PB * NB + b * NB + j) * 64 + lane] = acc[b0 + b][j];
+            __syncthreads();
+            for (int f = wave; f < PB * NB; f += KW) {
+                i32x4 one[1][1] = {{sums[f * 64 + lane]}};
+#pragma unroll
+                for (int q = 1; q < KW; ++q) one[0][0] += sums[(q * PB * NB + f) * 64 + lane];
+                quant_store_tile<1, 1>(a, t0 + 16 * (b0 + f / NB), n0 + 16 * (f % NB), one);
+            }
+        }
     }
 }
 
-template <int MB, int NB, int WAVES>
-void launch_rows(const QuantLinearArgs& a, hipStream_t st) {
+template <int MB, int NB, int KW, int NS>
+void launch_split(const QuantLinearArgs& a, hipStream_t st) {
     const int m_tiles = (a.rows + 16 * MB - 1) / (16 * MB), n_tiles = (a.cols + 16 * NB - 1) / (16 * NB);
-    hipLaunchKernelGGL((cats_quant_linear_rows<MB, NB, WAVES>), dim3(static_cast<unsigned>(m_tiles) * n_tiles),
-                       dim3(64 * WAVES), 0, st, a, m_tiles);
+    hipLaunchKernelGGL((cats_quant_linear_split<MB, NB, KW, NS>), dim3(static_cast<unsigned>(m_tiles) * n_tiles), dim3(64 * KW), 0,
+                       st, a, m_tiles, n_tiles);
 }
 
 // One wave moves one kilobyte: rows of 64 values in, an operand of the matrix instruction out.
@@ -95,12 +149,12 @@ bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
 void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
     if (a.rows < 1) return;
-    if (a.rows <= 16)
-        launch_rows<1, 1, 8>(a, st);
-    else if (a.rows >= 256 && a.x_ld < (1 << 23))
-        launch_quant_linear_tiles(a, n_cus, st);
-    else
-        launch_rows<4, 2, 4>(a, st);
+    static constexpr void (*LAUNCH[])(const QuantLinearArgs&, hipStream_t) = {
+        launch_split<1, 1, 8, 1>, launch_split<1, 2, 8, 1>, launch_split<2, 2, 8, 1>, launch_split<4, 2, 4, 2>, launch_split<4, 3, 4, 1>,
+        launch_split<4, 4, 4, 1>, launch_split<4, 6, 4, 1>, launch_split<6, 6, 4, 1>, launch_split<8, 4, 4, 1>, launch_split<8, 6, 4, 1>,
+        launch_split<8, 8, 4, 1>, launch_quant_tiles_half,  launch_quant_tiles};
+    static_assert(sizeof(LAUNCH) / sizeof(LAUNCH[0]) == N_QUANT_TILES, "one kernel for each tile");
+    LAUNCH[quant_tile_choice(a.rows, a.cols, n_cus)](a, st);
 }
 
 extern "C" {
@@ -127,6 +181,7 @@ int cats_quantized_linear(const int8_t* x, int64_t x_ld, const float* x_scale, c
         reinterpret_cast<uintptr_t>(y) % (y_type == CATS_F32 ? 4 : 2) != 0)
         return CATS_EINVAL;
     if (inner > CATS_QUANT_MAX_INNER || rows > CATS_QUANT_MAX_ROWS || cols > CATS_QUANT_MAX_ROWS ||
+        x_ld >= CATS_QUANT_MAX_LD ||                             // offsets inside a tile of X: fewer than 2^31
         static_cast<int64_t>(rows) * cols > (int64_t{1} << 33))   // threads of a launch: fewer than 2^32
         return CATS_ECAPACITY;
     if (rows == 0) return CATS_OK;

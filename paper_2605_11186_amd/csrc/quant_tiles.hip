@@ -6,12 +6,6 @@
 
 namespace {
 
-// 64 lanes copy 16 bytes each from base + their own offset to 1024 consecutive bytes of LDS (at byte `lds`), with no
-// register between.  Counted in vmcnt like a load; the compiler does not see it and waits for nothing on its account.
-__device__ __forceinline__ void copy_to_lds(const int8_t* base, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
-}
-
 // A workgroup of WM x WN waves owns a tile of BM = 16 WM MB rows of X and BN = 16 WN NB columns, a wave MB x NB blocks of
 // 16 x 16.  X passes through LDS in steps of 128 values of k, NS - 1 steps ahead; W's packed fragments go straight from
 // memory into the registers of the matrix instruction.
@@ -26,14 +20,8 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
-    // workgroup b runs on XCD b % 8: an XCD takes a run of tiles, in bands of 8 row tiles
-    const int total = m_tiles * n_tiles, xcd = blockIdx.x & 7, per = total >> 3, rem = total & 7;
-    const int id = xcd * per + min(xcd, rem) + (blockIdx.x >> 3);
-    constexpr int BAND = 4;
-    const int band = id / (BAND * n_tiles), in_band = id - band * BAND * n_tiles;
-    const int band_rows = min(BAND, m_tiles - band * BAND);
-    const int mt = __builtin_amdgcn_readfirstlane(band * BAND + in_band % band_rows), nt = __builtin_amdgcn_readfirstlane(in_band / band_rows);
-
+    int mt, nt;
+    quant_tile_of(m_tiles, n_tiles, mt, nt);
     const int steps = a.chunks >> 1;
     const int k_last = (a.inner - 1) / 16 * 16;
     const int n_rb = (a.cols + QPACK_ROWS - 1) / QPACK_ROWS;
@@ -142,7 +130,5 @@ void launch_tiles(const QuantLinearArgs& a, hipStream_t st) {
 
 }  // namespace
 
-void launch_quant_linear_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
-    (void)n_cus;
-    launch_tiles<2, 4, 8, 4, 4, 4>(a, st);
-}
+void launch_quant_tiles(const QuantLinearArgs& a, hipStream_t st) { launch_tiles<2, 4, 8, 4, 4, 4>(a, st); }
+void launch_quant_tiles_half(const QuantLinearArgs& a, hipStream_t st) { launch_tiles<2, 4, 4, 4, 4, 4>(a, st); }

@@ -208,7 +208,7 @@ def whole_numbers(rng, rows, cols, lo=-128, ld=None):
 
 
 def check_linear(x, sx, w, sw, y):
-    acc = x.cpu().double().numpy() @ w.cpu().double().numpy().T   # whole numbers below 2^53: exact
+    acc = f64(x.double() @ w.double().t().contiguous())   # whole numbers below 2^53: exact
     want = acc * f64(sx)[:, None] * f64(sw)[None, :]
     got = f64(y)
     tol = 3.01 * 2.0 ** -24 + (2.0 ** -8 if y.dtype == torch.bfloat16 else 0)
@@ -238,6 +238,19 @@ def run_linear(rows, cols, inner, dtype, x_ld=None, y_ld=None, seed=0):
     (1025, 511, 77), (2100, 300, 130)])
 def test_linear(rows, cols, inner, dtype):
     run_linear(rows, cols, inner, dtype)
+
+
+# one size for each tile that a product is cut into on 256 compute units (tests/test_quant_choice.py), none of them whole
+TILE_SIZES = {(16, 16): (13, 1003), (16, 32): (9, 4107), (32, 32): (30, 4107), (64, 32): (62, 4107), (64, 48): (57, 10007),
+              (64, 64): (254, 4077), (64, 96): (61, 21001), (96, 96): (95, 21001), (128, 64): (509, 4077),
+              (128, 96): (125, 21001), (128, 128): (1021, 4077), (128, 256): (2001, 4077), (256, 256): (4001, 4077)}
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("inner", [77, 1337])   # less than a step; several for each wave, the last one cut
+@pytest.mark.parametrize("tile", sorted(TILE_SIZES))
+def test_linear_every_tile(tile, inner, dtype):
+    run_linear(*TILE_SIZES[tile], inner, dtype)
 
 
 @pytest.mark.parametrize("rows", [1, 40, 130, 520])
@@ -296,11 +309,15 @@ def test_offsets_beyond_32_bits():
     cats.cats_quantize_rows(src, q, scale)
     check_rows(f64(src), q, scale, 0.0)
     w = whole_numbers(rng_of(9), 40, cols)
+    ld = cats.CATS_QUANT_MAX_LD - 16   # the longest stride of the product's x
+    x = torch.empty(rows * ld, dtype=torch.int8, device="cuda").as_strided((rows, cols), (ld, 1))
+    x.copy_(q)
+    q, ld = x, 1 << 30
     y = torch.empty(2 * ld + 64, device="cuda").as_strided((rows, 40), (ld, 1))
     sw = torch.full((40,), 1e-3, device="cuda")
     cats.cats_quantized_linear(q, scale, cats.cats_pack_quantized_matrix(w), sw, y)
     check_linear(q, scale, w, sw, y)
-    del big, q, y
+    del big, q, x, y
     inner, n = 16400, 131104   # 2.15e9 bytes
     w = torch.randint(-128, 128, (n, inner), dtype=torch.int8, device="cuda")
     wp = cats.cats_pack_quantized_matrix(w)

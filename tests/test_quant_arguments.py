@@ -63,7 +63,7 @@ def test_pack_quantized_matrix(changed, status):
     (dict(y_type=2), E), (dict(x=P + 8), E), (dict(x_ld=72), E), (dict(x_ld=48), E), (dict(y_ld=15), E), (dict(w=P + 8), E),
     (dict(y=P + 2), E), (dict(x_scale=P + 2), E), (dict(w_scale=P + 2), E), (dict(rows=-1), E), (dict(cols=0), E),
     (dict(inner=0), E), (dict(inner=BIG_INNER, x_ld=BIG_INNER // 16 * 16 + 16), CAP), (dict(rows=BIG_ROWS), CAP),
-    (dict(cols=BIG_ROWS, y_ld=BIG_ROWS), CAP), (dict(rows=2 ** 20, cols=2 ** 20, y_ld=2 ** 20), CAP),
+    (dict(cols=BIG_ROWS, y_ld=BIG_ROWS), CAP), (dict(x_ld=cats.CATS_QUANT_MAX_LD), CAP), (dict(rows=2 ** 20, cols=2 ** 20, y_ld=2 ** 20), CAP),
     (dict(rows=0), cats.CATS_OK)])
 def test_quantized_linear(changed, status):
     assert call("cats_quantized_linear", LINEAR, **changed) == status

@@ -1,0 +1,51 @@
+"""Which tile a product of 8-bit integers is cut into (host code, no GPU)."""
+import ctypes
+import re
+
+import pytest
+
+import host_shim
+from test_gpu_quant import TILE_SIZES
+
+SHIM = """
+#include "quant_choice.hpp"
+extern "C" {
+int n_tiles() { return N_QUANT_TILES; }
+int tile(int i, int what) { return what == 0 ? QUANT_TILES[i].bm : what == 1 ? QUANT_TILES[i].bn : QUANT_TILES[i].cost; }
+int choice(int rows, int cols, int n_cus) { return quant_tile_choice(rows, cols, n_cus); }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def rule():
+    return host_shim.build(SHIM)
+
+
+def tile(rule, rows, cols, n_cus=256):
+    i = rule.choice(rows, cols, n_cus)
+    return rule.tile(i, 0), rule.tile(i, 1)
+
+
+def test_every_tile_has_its_gpu_case(rule):
+    assert sorted(TILE_SIZES) == sorted((rule.tile(i, 0), rule.tile(i, 1)) for i in range(rule.n_tiles()))
+    for want, (rows, cols) in TILE_SIZES.items():
+        assert tile(rule, rows, cols) == want
+        assert rows % want[0] and cols % want[1]   # no size is a whole number of tiles
+
+
+def test_kernels_stand_in_the_order_of_the_tiles(rule):
+    """launch_quant_linear's list: <row blocks, column blocks, ...> of 16, then the two of the other kernel."""
+    text = (host_shim.CSRC / "quant_linear.hip").read_text()
+    built = [(16 * int(m), 16 * int(n)) for m, n in re.findall(r"launch_split<(\d), (\d), \d, \d>[,\s]", text)]
+    tiles = [(rule.tile(i, 0), rule.tile(i, 1)) for i in range(rule.n_tiles())]
+    assert built + [(128, 256), (256, 256)] == tiles
+
+
+def test_the_choice_costs_least(rule):
+    for rows in (1, 16, 17, 63, 64, 65, 128, 129, 500, 1024, 4096, 100000, 2 ** 21):
+        for cols in (1, 16, 100, 4096, 5120, 22016, 32000, 2 ** 21):
+            for n_cus in (1, 80, 256):
+                costs = [-(-(-(-rows // rule.tile(i, 0)) * -(-cols // rule.tile(i, 1))) // n_cus) * rule.tile(i, 2)
+                         for i in range(rule.n_tiles())]
+                assert costs[rule.choice(rows, cols, n_cus)] == min(costs)
