@@ -323,8 +323,8 @@ int cats_tree_attention_noalloc(const void *q, const cats_kv_layer *kv, const in
 /* ---- A decoder layer in 8-bit integers (the layers of the target verification pass for a target whose
  * weights and activations are held in 8 bits: half the bytes of the layer-weight stream).
  *
- * A row v of 8-bit integers carries one scale: q = v / scale rounded to whole numbers (ties to even; a quotient within
- * 2^-15 of a tie may go either way), -127 <= q <= 127, scale = max|v| / 127 and at least 2^-126.  A row that holds an
+ * A row v in 8-bit integers carries one scale: q = 127 v / max|v| rounded to whole numbers (ties to even; where v is itself
+ * computed, quotients within 2^-10 of a tie may go either way), -127 <= q <= 127, scale = max|v| / 127 and at least 2^-126.  A row that holds an
  * infinity or a NaN (for the norm also: whose sum of squares passes the range of float32) has q = 0 and scale = NaN; other rows do not
  * notice.  Weights are rows in this sense, one per output column.
  * Arithmetic before the rounding is float32, sums included.  Types of float inputs and outputs: CATS_F32, CATS_BF16.

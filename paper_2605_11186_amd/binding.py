@@ -366,89 +366,109 @@ def cats_lm_head_argmax(ctx, hidden, g_final, w_lm, argmax_out, logits_out=None,
                                          _dp(logits_out), _dp(argmax_out), _dp(margin_out), _stream(stream)))
 
 
-def _type_code(t):
-    """CATS_F32 or CATS_BF16 of a tensor."""
-    import torch
-    code = {torch.float32: CATS_F32, torch.bfloat16: CATS_BF16}.get(t.dtype)
-    if code is None:
-        raise CatsError(CATS_EINVAL, f"float32 or bfloat16 expected, got {t.dtype}")
-    return code
+class _Types:
+    """torch's types that the operators take (filled in by their first call: importing this module does not import torch)."""
+    f32 = bf16 = i8 = current_device = None
+    code = {}
+
+    @classmethod
+    def load(cls):
+        import torch
+        cls.f32, cls.bf16, cls.i8 = torch.float32, torch.bfloat16, torch.int8
+        cls.current_device = staticmethod(torch.cuda.current_device)
+        cls.code = {torch.float32: CATS_F32, torch.bfloat16: CATS_BF16}
+
+
+def _device_and_code(t):
+    """Device number of a tensor (-1: host memory) and CATS_F32, CATS_BF16 or None for its type."""
+    if not _Types.code:
+        _Types.load()
+    return t.get_device(), _Types.code.get(t.dtype)
+
+
+def _unfit(name, t, dtype, shape, device):
+    return CatsError(CATS_EINVAL, f"{name}: {dtype} {list(shape)} with neighbouring elements on device {device} expected, got "
+                                  f"{t.dtype} {list(t.shape)}, strides {list(t.stride())} on device {t.get_device()}")
 
 
 def _rows_of(name, t, dtype, rows, cols, device):
     """Checks of a [rows][cols] operand whose rows lie in one piece each; returns its row stride in elements."""
-    if t.dtype != dtype or t.shape != (rows, cols) or t.device != device:
-        raise CatsError(CATS_EINVAL, f"{name}: {dtype} [{rows}][{cols}] on {device} expected, got {t.dtype} "
-                                     f"{list(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.shape != (rows, cols) or t.get_device() != device:
+        raise _unfit(name, t, dtype, (rows, cols), device)
     ld, step = t.stride()
     if step != 1 and cols > 1:
-        raise CatsError(CATS_EINVAL, f"{name}: the elements of a row must be neighbours in memory")
+        raise _unfit(name, t, dtype, (rows, cols), device)
     # the stride of a single row says nothing: any that suits a row of this length will do
-    return ld if rows > 1 else max(ld, (cols + 15) // 16 * 16)
+    return ld if rows > 1 else (cols + 15) // 16 * 16
 
 
 def _vector(name, t, dtype, n, device):
-    if t.dtype != dtype or t.shape != (n,) or t.device != device or (n > 1 and t.stride(0) != 1):
-        raise CatsError(CATS_EINVAL, f"{name}: contiguous {dtype} [{n}] on {device} expected, got {t.dtype} "
-                                     f"{list(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
+        raise _unfit(name, t, dtype, (n,), device)
+    return t.data_ptr()
 
 
-def _current(device):
-    """The operators run on the current device: refuse tensors that live elsewhere."""
-    import torch
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise CatsError(CATS_EINVAL, f"tensors on {device}, which is not the current device")
+def _current(device, stream):
+    """The operators run on the current device: refuse tensors and streams that belong elsewhere.  Returns the stream's handle."""
+    if device < 0 or device != _Types.current_device():
+        raise CatsError(CATS_EINVAL, f"tensors on device {device}, which is not the current GPU")
+    if stream is None:
+        return None
+    if getattr(stream, "device_index", device) != device:
+        raise CatsError(CATS_EINVAL, f"stream of device {stream.device_index}, tensors on device {device}")
+    return getattr(stream, "cuda_stream", stream)
+
+
+def _floats(name, code, t):
+    if code is None:
+        raise CatsError(CATS_EINVAL, f"{name}: float32 or bfloat16 expected, got {t.dtype}")
+    return code
 
 
 def cats_quantize_rows(src, q_out, scale_out, stream=None):
     """Rows of src (float32 or bfloat16 [rows][cols]) as int8 with one float32 scale each."""
-    import torch
-    (rows, cols), dev = src.shape, src.device
-    code, ld = _type_code(src), _rows_of("src", src, src.dtype, rows, cols, dev)
-    q_ld = _rows_of("q_out", q_out, torch.int8, rows, cols, dev)
-    _vector("scale_out", scale_out, torch.float32, rows, dev)
-    _current(dev)
-    if rows == 0:
-        return
-    _check(library().cats_quantize_rows(src.data_ptr(), code, ld, rows, cols, q_out.data_ptr(), q_ld,
-                                        scale_out.data_ptr(), _stream(stream)))
+    rows, cols = src.shape
+    dev, code = _device_and_code(src)
+    code, ld = _floats("src", code, src), _rows_of("src", src, src.dtype, rows, cols, dev)
+    q_ld = _rows_of("q_out", q_out, _Types.i8, rows, cols, dev)
+    scale = _vector("scale_out", scale_out, _Types.f32, rows, dev)
+    st = _current(dev, stream)
+    if rows:
+        _check(library().cats_quantize_rows(src.data_ptr(), code, ld, rows, cols, q_out.data_ptr(), q_ld, scale, st))
 
 
 def cats_rmsnorm_quantize(x, gain, eps: float, q_out, scale_out, delta=None, x_out=None, stream=None):
     """x (float32 [rows][cols]) plus delta, normalised, times gain, as int8 rows with scales.  With delta the sum
     goes to x_out, or back to x if none is given."""
-    import torch
-    (rows, cols), dev = x.shape, x.device
-    ld = _rows_of("x", x, torch.float32, rows, cols, dev)
-    _vector("gain", gain, torch.bfloat16, cols, dev)
-    q_ld = _rows_of("q_out", q_out, torch.int8, rows, cols, dev)
-    _vector("scale_out", scale_out, torch.float32, rows, dev)
+    rows, cols = x.shape
+    dev, _ = _device_and_code(x)
+    ld = _rows_of("x", x, _Types.f32, rows, cols, dev)
+    g = _vector("gain", gain, _Types.bf16, cols, dev)
+    q_ld = _rows_of("q_out", q_out, _Types.i8, rows, cols, dev)
+    scale = _vector("scale_out", scale_out, _Types.f32, rows, dev)
     d_ptr, d_code, d_ld, o_ptr, o_ld = None, 0, 0, None, 0
     if delta is not None:
-        d_ptr, d_code, d_ld = delta.data_ptr(), _type_code(delta), _rows_of("delta", delta, delta.dtype, rows, cols, dev)
+        d_code, d_ld = _floats("delta", _Types.code.get(delta.dtype), delta), _rows_of("delta", delta, delta.dtype, rows, cols, dev)
         out = x if x_out is None else x_out
-        o_ptr, o_ld = out.data_ptr(), _rows_of("x_out", out, torch.float32, rows, cols, dev)
+        d_ptr, o_ptr, o_ld = delta.data_ptr(), out.data_ptr(), _rows_of("x_out", out, _Types.f32, rows, cols, dev)
     elif x_out is not None:
         raise CatsError(CATS_EINVAL, "x_out without delta: x does not change")
-    _current(dev)
-    if rows == 0:
-        return
-    _check(library().cats_rmsnorm_quantize(x.data_ptr(), ld, d_ptr, d_code, d_ld, gain.data_ptr(), eps, rows, cols, o_ptr,
-                                           o_ld, q_out.data_ptr(), q_ld, scale_out.data_ptr(), _stream(stream)))
+    st = _current(dev, stream)
+    if rows:
+        _check(library().cats_rmsnorm_quantize(x.data_ptr(), ld, d_ptr, d_code, d_ld, g, eps, rows, cols, o_ptr, o_ld,
+                                               q_out.data_ptr(), q_ld, scale, st))
 
 
 def cats_swiglu_quantize(gate_up, q_out, scale_out, stream=None):
     """silu(gate) * up of gate_up (float32 or bfloat16 [rows][2 cols], gate | up) as int8 rows with scales."""
-    import torch
-    (rows, cols), dev = q_out.shape, gate_up.device
-    code, ld = _type_code(gate_up), _rows_of("gate_up", gate_up, gate_up.dtype, rows, 2 * cols, dev)
-    q_ld = _rows_of("q_out", q_out, torch.int8, rows, cols, dev)
-    _vector("scale_out", scale_out, torch.float32, rows, dev)
-    _current(dev)
-    if rows == 0:
-        return
-    _check(library().cats_swiglu_quantize(gate_up.data_ptr(), code, ld, rows, cols, q_out.data_ptr(), q_ld,
-                                          scale_out.data_ptr(), _stream(stream)))
+    rows, cols = q_out.shape
+    dev, code = _device_and_code(gate_up)
+    code, ld = _floats("gate_up", code, gate_up), _rows_of("gate_up", gate_up, gate_up.dtype, rows, 2 * cols, dev)
+    q_ld = _rows_of("q_out", q_out, _Types.i8, rows, cols, dev)
+    scale = _vector("scale_out", scale_out, _Types.f32, rows, dev)
+    st = _current(dev, stream)
+    if rows:
+        _check(library().cats_swiglu_quantize(gate_up.data_ptr(), code, ld, rows, cols, q_out.data_ptr(), q_ld, scale, st))
 
 
 def cats_packed_quantized_bytes(rows: int, cols: int) -> int:
@@ -458,30 +478,28 @@ def cats_packed_quantized_bytes(rows: int, cols: int) -> int:
 def cats_pack_quantized_matrix(src, stream=None):
     """Packed copy of int8 weights [out][in] (new device tensor, int8)."""
     import torch
-    (rows, cols), dev = src.shape, src.device
+    rows, cols = src.shape
+    dev, _ = _device_and_code(src)
     ld = _rows_of("src", src, torch.int8, rows, cols, dev)
-    _current(dev)
-    dst = torch.empty(cats_packed_quantized_bytes(rows, cols), dtype=torch.int8, device=dev)
-    _check(library().cats_pack_quantized_matrix(src.data_ptr(), ld, rows, cols, dst.data_ptr(), _stream(stream)))
+    st = _current(dev, stream)
+    dst = torch.empty(cats_packed_quantized_bytes(rows, cols), dtype=torch.int8, device=src.device)
+    _check(library().cats_pack_quantized_matrix(src.data_ptr(), ld, rows, cols, dst.data_ptr(), st))
     return dst
 
 
 def cats_quantized_linear(x, x_scale, w_packed, w_scale, out, stream=None):
     """out [rows][cols] (float32 or bfloat16) = (x . W) * x_scale * w_scale for int8 x [rows][inner] and packed int8 W [cols][inner]."""
-    import torch
-    (rows, inner), (_, cols), dev = x.shape, out.shape, x.device
-    code, ld = _type_code(out), _rows_of("x", x, torch.int8, rows, inner, dev)
+    (rows, inner), (_, cols) = x.shape, out.shape
+    dev, code = _device_and_code(out)
+    code, ld = _floats("out", code, out), _rows_of("x", x, _Types.i8, rows, inner, dev)
     y_ld = _rows_of("out", out, out.dtype, rows, cols, dev)
-    _vector("x_scale", x_scale, torch.float32, rows, dev)
-    _vector("w_scale", w_scale, torch.float32, cols, dev)
+    sx, sw = _vector("x_scale", x_scale, _Types.f32, rows, dev), _vector("w_scale", w_scale, _Types.f32, cols, dev)
+    w = _vector("w_packed", w_packed, _Types.i8, (cols + 15) // 16 * ((inner + 255) // 256) * 4096, dev)
     if inner % 16 and x.untyped_storage().nbytes() < x.storage_offset() + (rows - 1) * ld + (inner + 15) // 16 * 16:
         raise CatsError(CATS_EINVAL, "x: its last row must be readable up to a multiple of 16 bytes")
-    _vector("w_packed", w_packed, torch.int8, (cols + 15) // 16 * ((inner + 255) // 256) * 4096, dev)
-    _current(dev)
-    if rows == 0:
-        return
-    _check(library().cats_quantized_linear(x.data_ptr(), ld, x_scale.data_ptr(), w_packed.data_ptr(), w_scale.data_ptr(),
-                                           out.data_ptr(), code, y_ld, rows, cols, inner, _stream(stream)))
+    st = _current(dev, stream)
+    if rows:
+        _check(library().cats_quantized_linear(x.data_ptr(), ld, sx, w, sw, out.data_ptr(), code, y_ld, rows, cols, inner, st))
 
 
 def cats_profile_gemm(ctx, enable: bool):

@@ -191,14 +191,27 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
     const bool finite = top < 0x7F800000u;
     const float most = fmaxf(__uint_as_float(top), 127.f * SCALE_MIN);
     if (tid == 0) a.scale[t] = finite ? most / 127.f : NAN;
-    const float inv = 127.f / most;
-    // v * inv + 1.5 * 2^23: the sum's last bits are the nearest whole number in two's complement (one rounding, ties to even)
+    // y + 1.5 * 2^23: the sum's last bits are the whole number nearest to y in two's complement (ties to even)
+    constexpr float WHOLE = 12582912.f;
+    // ROWS_PLAIN: y = 127 v / most as a correctly rounded quotient (by one correction), so that ties, which are common among bf16
+    // values, are seen: by the power of two p, most p lies in [1, 4) and no product leaves the range.  Computed rows have no ties
+    // worth the three instructions a value.
+    const float p = __uint_as_float(max(0x7F000000u - (__float_as_uint(most) & 0x7F800000u), 0x00800000u));
+    const float den = KIND == ROWS_PLAIN ? most * p : most, mul = KIND == ROWS_PLAIN ? 127.f * p : 127.f / most, rden = 1.f / den;
+    auto whole = [&](float v) {
+        if constexpr (KIND == ROWS_PLAIN) {
+            const float z = v * mul, y = z * rden;
+            return __float_as_uint(fmaf(fmaf(-y, den, z), rden, y) + WHOLE);
+        } else {
+            return __float_as_uint(fmaf(v, mul, WHOLE));
+        }
+    };
     int8_t* q = a.q + t * a.q_ld;
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
         uint32_t b[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) b[e] = finite ? __float_as_uint(fmaf(v[j][e], inv, 12582912.f)) & 0xFFu : 0u;
+        for (int e = 0; e < 8; ++e) b[e] = finite ? whole(v[j][e]) & 0xFFu : 0u;
         if constexpr (VEC) {
             if (in[j][0])
                 *reinterpret_cast<uint2*>(q + place<TPR, VEC>(tid, j, 0)) =
@@ -235,17 +248,17 @@ static_assert(CATS_QUANT_MAX_ROWS <= (1 << 21), "threads of a launch: fewer than
 static_assert(CATS_QUANT_MAX_COLS == 1024 * 8 * 8, "the longest row fills the largest workgroup's registers");
 
 // Whole pieces of 8 values: no row starts or ends inside one, and rows stay aligned.
-bool whole(const void* p, int64_t ld, size_t size) {
+bool whole_pieces(const void* p, int64_t ld, size_t size) {
     const size_t piece = size == 4 ? 16 : 8 * size;   // float32 pieces are two loads of 16 bytes
     return (reinterpret_cast<uintptr_t>(p) | static_cast<uint64_t>(ld) * size) % piece == 0;
 }
 
 template <int KIND, class T, class D>
 void by_alignment(const QuantRowsArgs& a, int n_cus, hipStream_t st) {
-    bool vec = a.cols % 8 == 0 && whole(a.src, a.src_ld, sizeof(T)) && whole(a.q, a.q_ld, 1);
-    if (KIND == ROWS_NORM) vec = vec && whole(a.gain, 0, 2);
+    bool vec = a.cols % 8 == 0 && whole_pieces(a.src, a.src_ld, sizeof(T)) && whole_pieces(a.q, a.q_ld, 1);
+    if (KIND == ROWS_NORM) vec = vec && whole_pieces(a.gain, 0, 2);
     if (KIND == ROWS_NORM && sizeof(D) < 8)
-        vec = vec && whole(a.delta, a.delta_ld, sizeof(D)) && whole(a.x_out, a.x_out_ld, 4);
+        vec = vec && whole_pieces(a.delta, a.delta_ld, sizeof(D)) && whole_pieces(a.x_out, a.x_out_ld, 4);
     if (vec)
         by_size<KIND, T, D, true>(a, n_cus, st);
     else

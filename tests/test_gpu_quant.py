@@ -156,6 +156,20 @@ def test_whole_numbers_and_ties_to_even():
         assert q[0, :12].tolist() == [127, 0, 2, 2, 0, -2, -2, 126, -126, -127, 3, 0]
 
 
+def test_ties_among_bf16_values():
+    """127 v / max|v| of bf16 values is a tie or next to none: |2 * 127 v - k max|v||, k odd, is a whole multiple of the values' last
+    bits, so the quotient is a tie or at least 2^-16 / 2 from one relative to it, and float64 tells which."""
+    src = normal(rng_of(12), 400, 2048, torch.bfloat16)
+    src[100:200] *= 1e30
+    src[200:300] *= 1e-30
+    q, scale = torch.empty(400, 2048, dtype=torch.int8, device="cuda"), torch.empty(400, device="cuda")
+    cats.cats_quantize_rows(src, q, scale)
+    v = f64(src)
+    y = v * 127 / np.abs(v).max(1, keepdims=True)
+    assert (np.abs(y) % 1 == 0.5).sum() > 100   # there are some
+    assert np.array_equal(f64(q), np.rint(y))
+
+
 @pytest.mark.parametrize("cols", [5, 64, 4096, 9000])
 def test_rows_of_zeros_tiny_huge_and_not_numbers(cols):
     rng = rng_of(5, cols)
