@@ -377,6 +377,26 @@ int cats_pack_quantized_matrix(const int8_t *src, int64_t src_ld, int32_t rows, 
 int cats_quantized_linear(const int8_t *x, int64_t x_ld, const float *x_scale, const int8_t *w_packed, const float *w_scale,
                           void *y, int32_t y_type, int64_t y_ld, int32_t rows, int32_t cols, int32_t inner, void *stream);
 
+/* One decoder layer with 8-bit weights: cats_pack_quantized_matrix outputs and the scales of their rows.  w_qkv: [3 hidden][hidden]
+ * (q, k, v rows in this order), w_o: [hidden][hidden], w_gate_up: [2 ffn][hidden] (gate rows, then up rows), w_down: [hidden][ffn];
+ * g_attn, g_ffn: RMSNorm gains, bf16 [hidden]. */
+typedef struct {
+    const int8_t *w_qkv, *w_o, *w_gate_up, *w_down;
+    const float *s_qkv, *s_o, *s_gate_up, *s_down;
+    const void *g_attn, *g_ffn;
+} cats_quantized_layer;
+
+/* Layers [layer_begin, layer_end) of `layers` (HOST array indexed by layer) over all T tree nodes, as cats_verify_layer runs
+ * them, with every product's input in 8 bits: the operators above, and rotation, cache append and tree attention as in
+ * the other calls (the cache is bf16, queries and the call's own rows carry about 16 mantissa bits).  The attention output is rounded to bf16 before
+ * it is quantised, the other products' outputs stay float32.  hidden: float32 [T][hidden], 16-byte aligned, in/out.  kv: HOST array
+ * indexed by layer.  The context's packed_weights plays no part, and cats_profile_gemm does not count these products.
+ * A whole step: cats_set_tree, embedding rows in hidden, this call, cats_lm_head_argmax, cats_accept_and_compact.
+ * CATS_EINVAL: a bad layer range, a NULL or misaligned pointer in a layer of the range (weights 16 bytes, scales 4, gains 2), hidden NULL or
+ * misaligned; CATS_ECAPACITY: ffn above CATS_QUANT_MAX_COLS; an empty range enqueues nothing. */
+int cats_verify_layers_quantized(cats_ctx *ctx, const cats_quantized_layer *layers, int32_t layer_begin, int32_t layer_end,
+                                 float *hidden, const cats_kv_layer *kv, int32_t ctx_len, void *stream);
+
 /* Measurement aid for the weight-streaming products (the layer-weight pass of the
  * "Target verification pass"; a product that rotates and appends to the cache, or applies SwiGLU,
  * is timed with that step): while enabled, every product launch made through

@@ -25,7 +25,8 @@ __all__ = ["CATS_MAX_TREE", "CATS_MAX_DEPTH", "CatsError", "ModelDesc", "LayerWe
            "accept_result_from_tensor", "CATS_OK", "CATS_EINVAL", "CATS_ECAPACITY", "CATS_ESTATE",
            "CATS_EHIP", "CATS_F32", "CATS_BF16", "CATS_QUANT_MAX_COLS", "CATS_QUANT_MAX_ROWS", "CATS_QUANT_MAX_LD", "CATS_QUANT_MAX_INNER",
            "cats_quantize_rows", "cats_rmsnorm_quantize", "cats_swiglu_quantize",
-           "cats_packed_quantized_bytes", "cats_pack_quantized_matrix", "cats_quantized_linear"]
+           "cats_packed_quantized_bytes", "cats_pack_quantized_matrix", "cats_quantized_linear",
+           "QuantizedLayer", "cats_verify_layers_quantized", "quantize_layer", "quantized_layer_array"]
 
 CATS_MAX_TREE = 128
 CATS_MAX_DEPTH = 16
@@ -59,6 +60,11 @@ class ModelDesc(C.Structure):
 class LayerWeights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in
                 ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down", "g_attn", "g_ffn")]
+
+
+class QuantizedLayer(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in
+                ("w_qkv", "w_o", "w_gate_up", "w_down", "s_qkv", "s_o", "s_gate_up", "s_down", "g_attn", "g_ffn")]
 
 
 class KVLayer(C.Structure):
@@ -116,6 +122,8 @@ _SIGNATURES = {
                          C.c_void_p, C.c_void_p],
     "cats_tree_attention_noalloc": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                     C.c_int32, C.c_int32, C.c_void_p, C.c_void_p],
+    "cats_verify_layers_quantized": [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32,
+                                     C.c_void_p],
     "cats_quantize_rows": [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p,
                            C.c_void_p],
     "cats_rmsnorm_quantize": [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_float, C.c_int32,
@@ -500,6 +508,36 @@ def cats_quantized_linear(x, x_scale, w_packed, w_scale, out, stream=None):
     st = _current(dev, stream)
     if rows:
         _check(library().cats_quantized_linear(x.data_ptr(), ld, sx, w, sw, out.data_ptr(), code, y_ld, rows, cols, inner, st))
+
+
+def quantize_layer(tensors: dict) -> dict:
+    """A layer dict (row-major bf16 matrices wq .. w_down, gains) as 8-bit weights with scales, packed: the fields of
+    cats_quantized_layer as device tensors.  Works on torch's current stream."""
+    import torch
+    stream = torch.cuda.current_stream()
+    out = {"g_attn": tensors["g_attn"], "g_ffn": tensors["g_ffn"]}
+    for name, parts in (("qkv", ("wq", "wk", "wv")), ("o", ("wo",)), ("gate_up", ("w_gate", "w_up")), ("down", ("w_down",))):
+        w = torch.cat([tensors[p] for p in parts])
+        q = torch.empty(w.shape, dtype=torch.int8, device=w.device)
+        s = torch.empty(w.shape[0], dtype=torch.float32, device=w.device)
+        cats_quantize_rows(w, q, s, stream=stream)
+        out["w_" + name], out["s_" + name] = cats_pack_quantized_matrix(q, stream=stream), s
+    return out
+
+
+def quantized_layer_array(layer_dicts):
+    """QuantizedLayer array from quantize_layer's dicts (kept alive by the caller)."""
+    arr = (QuantizedLayer * len(layer_dicts))()
+    for i, t in enumerate(layer_dicts):
+        for n, _ in QuantizedLayer._fields_:
+            setattr(arr[i], n, t[n].data_ptr())
+    return arr
+
+
+def cats_verify_layers_quantized(ctx, layers_arr, layer_begin: int, layer_end: int, hidden, kv_arr, ctx_len: int, stream=None):
+    """Layers in 8 bits over the tree's nodes; hidden (float32 [T][hidden]) in and out."""
+    _check(library().cats_verify_layers_quantized(ctx, layers_arr, int(layer_begin), int(layer_end), _dp(hidden), kv_arr,
+                                                  int(ctx_len), _stream(stream)))
 
 
 def cats_profile_gemm(ctx, enable: bool):

@@ -3,10 +3,12 @@
 // through the commit step).
 #include <algorithm>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 
 #include "common.hpp"
+#include "quant.hpp"
 
 constexpr int CATS_PROF_MAX = 1024;  // GEMM launches that can be timed between two reads
 
@@ -68,6 +70,9 @@ struct cats_ctx {
     // probability of its token at its parent, the threshold there, and the decision
     float *typ_lse = nullptr, *typ_entropy = nullptr, *typ_slice = nullptr, *typ_prob = nullptr, *typ_thr = nullptr;
     uint8_t* typ_edge = nullptr;
+    // layers in 8 bits: scales of the rows in c->xn / c->hact (which then hold bytes), and sums of squares that stay zero, with
+    // which the rotation step takes q|k|v as they are
+    float *qscale, *ss_zero;   // [max_tree], [max_tree][SS_STRIDE]
     char* flat;      // the single allocation behind all of the above
     // offload regime: copy stream and the events that order it against the compute stream
     hipStream_t copy_stream;
@@ -477,6 +482,86 @@ void finish_row(cats_ctx* c, float* dst, const void* gain, hipStream_t st) {
     c->row.pend = nullptr;
 }
 
+// ---- layers in 8 bits.  Rows in front of a product lie in c->xn (hidden columns) or c->hact (ffn), with their scales in
+// c->qscale; every product leaves float32 rows in c->part.
+QuantRowsArgs quant_rows(const cats_ctx* c, const void* src, int64_t src_ld, int cols, void* q) {
+    QuantRowsArgs a{};
+    a.src = src;
+    a.src_ld = src_ld;
+    a.src_type = CATS_F32;
+    a.rows = c->rows;
+    a.cols = cols;
+    a.q = static_cast<int8_t*>(q);
+    a.q_ld = cols;
+    a.scale = c->qscale;
+    return a;
+}
+// c->xn = rmsnorm(x + delta) * gain in 8 bits, x += delta; delta: the rows in c->part, or none
+void enqueue_norm_quantized(cats_ctx* c, float* x, bool delta, const void* gain, hipStream_t st) {
+    const int H = c->d.hidden;
+    QuantRowsArgs a = quant_rows(c, x, H, H, c->xn);
+    a.delta = delta ? c->part : nullptr;
+    a.delta_type = CATS_F32;
+    a.delta_ld = H;
+    a.gain = static_cast<const bf16_t*>(gain);
+    a.eps = c->d.rms_eps;
+    a.x_out = delta ? x : nullptr;
+    a.x_out_ld = H;
+    launch_quant_rows(a, ROWS_NORM, c->n_cus, st);
+}
+void enqueue_linear_quantized(cats_ctx* c, const void* q, int inner, const int8_t* w, const float* w_scale, int cols, hipStream_t st) {
+    QuantLinearArgs a{};
+    a.x = static_cast<const int8_t*>(q);
+    a.x_ld = inner;
+    a.x_scale = c->qscale;
+    a.w = w;
+    a.w_scale = w_scale;
+    a.y = c->part;
+    a.y_type = CATS_F32;
+    a.y_ld = cols;
+    a.rows = c->rows;
+    a.cols = cols;
+    a.inner = inner;
+    a.chunks = qpack_chunks(inner);
+    launch_quant_linear(a, c->n_cus, st);
+}
+// One layer; delta: the layer before has left its last product in c->part, still to be added to x, as this one does.
+void enqueue_layer_quantized(cats_ctx* c, const cats_quantized_layer* w, float* x, bool delta, const cats_kv_layer* kv, int ctx_len,
+                             hipStream_t st) {
+    const int H = c->d.hidden, F = c->d.ffn;
+    enqueue_norm_quantized(c, x, delta, w->g_attn, st);
+    enqueue_linear_quantized(c, c->xn, H, w->w_qkv, w->s_qkv, 3 * H, st);
+    QkvRopeArgs qa;
+    qa.part = c->part;
+    qa.plan = GemmPlan{1, GEMM_KC, 1, 1, 1};   // one complete piece
+    qa.ns = NormScale{c->ss_zero, (H + SS_COLS - 1) / SS_COLS, H, 1.f};   // norm factor 1 / sqrt(0 + 1)
+    qa.cs = c->rope_cs;
+    qa.q = c->q;
+    qa.q_lo = c->q_lo;
+    qa.kc = static_cast<bf16_t*>(kv->k);
+    qa.vt = static_cast<bf16_t*>(kv->v);
+    qa.T = c->rows;
+    qa.H = H;
+    qa.nh = c->d.n_heads;
+    qa.d = c->d.head_dim;
+    qa.max_ctx = c->d.max_ctx;
+    qa.row0 = ctx_len;
+    qa.k_lo = c->k_lo;
+    qa.vt_lo = c->vt_lo;
+    qa.win0 = ctx_len % ATTN_KB;
+    launch_qkv_rope(qa, st);
+    // bf16 in front of 8 bits: its last bit is 2^-8 of a value, the step of the row 2^-7 of the largest one
+    enqueue_attention(c, c->q, c->q_lo, kv, ctx_len, c->attn, nullptr, true, st);
+    QuantRowsArgs a = quant_rows(c, c->attn, H, H, c->xn);
+    a.src_type = CATS_BF16;
+    launch_quant_rows(a, ROWS_PLAIN, c->n_cus, st);
+    enqueue_linear_quantized(c, c->xn, H, w->w_o, w->s_o, H, st);
+    enqueue_norm_quantized(c, x, true, w->g_ffn, st);
+    enqueue_linear_quantized(c, c->xn, H, w->w_gate_up, w->s_gate_up, 2 * F, st);
+    launch_quant_rows(quant_rows(c, c->part, 2 * static_cast<int64_t>(F), F, c->hact), ROWS_SWIGLU, c->n_cus, st);
+    enqueue_linear_quantized(c, c->hact, F, w->w_down, w->s_down, H, st);
+}
+
 RopeTableArgs rope_table_args(const cats_ctx* c, int ctx_len) {
     RopeTableArgs r;
     r.depth = c->depth;
@@ -672,6 +757,7 @@ int cats_create(const cats_model_desc* desc, cats_ctx** out) {
     const size_t o_wb = take(static_cast<size_t>(c->n_cus) * 4), o_wi = take(static_cast<size_t>(c->n_cus) * 4);
     const size_t o_tl = take(Tm * 4), o_te = take(Tm * 4), o_ts = take(Tm * ARGMAX_SLICES * 3 * 4);
     const size_t o_tp = take(Tm * 4), o_tt = take(Tm * 4), o_tg = take(Tm);
+    const size_t o_qs = take(Tm * 4), o_sz = take(Tm * SS_STRIDE * 4);   // zero from the memset below
     hipError_t e = hipMalloc(reinterpret_cast<void**>(&c->flat), off);
     if (e != hipSuccess) {
         delete c;
@@ -724,6 +810,8 @@ int cats_create(const cats_model_desc* desc, cats_ctx** out) {
     c->typ_prob = reinterpret_cast<float*>(b + o_tp);
     c->typ_thr = reinterpret_cast<float*>(b + o_tt);
     c->typ_edge = reinterpret_cast<uint8_t*>(b + o_tg);
+    c->qscale = reinterpret_cast<float*>(b + o_qs);
+    c->ss_zero = reinterpret_cast<float*>(b + o_sz);
     *out = c;
     return CATS_OK;
 }
@@ -797,6 +885,46 @@ int cats_verify_layer(cats_ctx* ctx, const cats_layer_weights* w, float* hidden,
     } else {
         enqueue_layer(ctx, w, hidden, kv, ctx_len, nullptr, false, st);
     }
+    HIP_TRY(hipGetLastError());
+    return CATS_OK;
+}
+
+int cats_verify_layers_quantized(cats_ctx* ctx, const cats_quantized_layer* layers, int32_t layer_begin, int32_t layer_end,
+                                 float* hidden, const cats_kv_layer* kv, int32_t ctx_len, void* stream) {
+    const int rc = check_ctx_len(ctx, ctx_len);
+    if (rc != CATS_OK) return rc;
+    if (layer_begin < 0 || layer_end < layer_begin || layer_end > ctx->d.n_layers || !hidden || !aligned16(hidden)) return CATS_EINVAL;
+    if (layer_end == layer_begin) return CATS_OK;
+    if (!layers || !kv_ok(kv, layer_begin, layer_end)) return CATS_EINVAL;
+    if (ctx->d.ffn > CATS_QUANT_MAX_COLS) return CATS_ECAPACITY;
+    for (int l = layer_begin; l < layer_end; ++l) {
+        const cats_quantized_layer& w = layers[l];
+        for (const int8_t* p : {w.w_qkv, w.w_o, w.w_gate_up, w.w_down})
+            if (!p || !aligned16(p)) return CATS_EINVAL;
+        for (const float* p : {w.s_qkv, w.s_o, w.s_gate_up, w.s_down})
+            if (!p || reinterpret_cast<uintptr_t>(p) % 4 != 0) return CATS_EINVAL;
+        for (const void* p : {w.g_attn, w.g_ffn})
+            if (!p || reinterpret_cast<uintptr_t>(p) % 2 != 0) return CATS_EINVAL;
+    }
+    hipStream_t st = as_stream(stream);
+    launch_rope_table(rope_table_args(ctx, ctx_len), st);
+    for (int l = layer_begin; l < layer_end; ++l)
+        enqueue_layer_quantized(ctx, &layers[l], hidden, l > layer_begin, &kv[l], ctx_len, st);
+    ResidualNormArgs rn;   // the last layer's product
+    rn.x = hidden;
+    rn.x_in = nullptr;
+    rn.embed = nullptr;
+    rn.token = nullptr;
+    rn.part = ctx->part;
+    rn.plan = GemmPlan{1, GEMM_KC, 1, 1, 1};
+    rn.gain = nullptr;
+    rn.xn = ctx->xn;
+    rn.xn_lo = ctx->xn_lo;
+    rn.ss = ctx->ss;
+    rn.T = ctx->rows;
+    rn.H = ctx->d.hidden;
+    rn.eps = ctx->d.rms_eps;
+    launch_residual_norm(rn, st);
     HIP_TRY(hipGetLastError());
     return CATS_OK;
 }
