@@ -507,7 +507,7 @@ void enqueue_norm_quantized(cats_ctx* c, float* x, bool delta, const void* gain,
     a.eps = c->d.rms_eps;
     a.x_out = delta ? x : nullptr;
     a.x_out_ld = H;
-    launch_quant_rows(a, ROWS_NORM, c->n_cus, st);
+    launch_quant_rows(a, ROWS_NORM, st);
 }
 void enqueue_linear_quantized(cats_ctx* c, const void* q, int inner, const int8_t* w, const float* w_scale, int cols, hipStream_t st) {
     QuantLinearArgs a{};
@@ -554,11 +554,11 @@ void enqueue_layer_quantized(cats_ctx* c, const cats_quantized_layer* w, float* 
     enqueue_attention(c, c->q, c->q_lo, kv, ctx_len, c->attn, nullptr, true, st);
     QuantRowsArgs a = quant_rows(c, c->attn, H, H, c->xn);
     a.src_type = CATS_BF16;
-    launch_quant_rows(a, ROWS_PLAIN, c->n_cus, st);
+    launch_quant_rows(a, ROWS_PLAIN, st);
     enqueue_linear_quantized(c, c->xn, H, w->w_o, w->s_o, H, st);
     enqueue_norm_quantized(c, x, true, w->g_ffn, st);
     enqueue_linear_quantized(c, c->xn, H, w->w_gate_up, w->s_gate_up, 2 * F, st);
-    launch_quant_rows(quant_rows(c, c->part, 2 * static_cast<int64_t>(F), F, c->hact), ROWS_SWIGLU, c->n_cus, st);
+    launch_quant_rows(quant_rows(c, c->part, 2 * static_cast<int64_t>(F), F, c->hact), ROWS_SWIGLU, st);
     enqueue_linear_quantized(c, c->hact, F, w->w_down, w->s_down, H, st);
 }
 

@@ -21,7 +21,7 @@ struct QuantRowsArgs {
     int src_type, delta_type;   // CATS_F32, CATS_BF16
 };
 // kind: ROWS_*.  Nothing is enqueued for no rows.
-void launch_quant_rows(const QuantRowsArgs& a, int kind, int n_cus, hipStream_t st);
+void launch_quant_rows(const QuantRowsArgs& a, int kind, hipStream_t st);
 
 // ---------------------------------------------------------------- product
 // Packed 8-bit weights: rows in blocks of 16 and columns in chunks of 64, a multiple of four of them, filled up with zeros; the
@@ -106,6 +106,3 @@ __device__ __forceinline__ void quant_store_tile(const QuantLinearArgs& a, int t
         }
     }
 }
-
-// Compute units of the current device (0: it could not be asked).
-int quant_cus();

@@ -3,6 +3,7 @@
 // The sums are whole numbers in 32 bits and exact (inner <= CATS_QUANT_MAX_INNER), so neither the order of the
 // summation nor the split of the work changes a result.
 #include <algorithm>
+#include <atomic>
 
 #include "quant.hpp"
 #include "quant_choice.hpp"
@@ -144,6 +145,19 @@ int64_t frags_of(int32_t rows, int32_t cols) {
 }
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
+// Compute units of the current device (0: it could not be asked).
+int quant_cus() {
+    constexpr int MAX_DEVICES = 64;
+    static std::atomic<int> known[MAX_DEVICES];   // zero: not asked yet
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) return 0;
+    n = known[dev].load(std::memory_order_relaxed);
+    if (n) return n;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return 0;
+    known[dev].store(n, std::memory_order_relaxed);
+    return n;
+}
 
 }  // namespace
 

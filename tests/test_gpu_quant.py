@@ -65,7 +65,8 @@ def norm_of(x, gain):
 
 # every number of threads and pieces a row is cut into, both sides of each border, rows of one value
 SIZES = [(1, 1), (3, 7), (5, 8), (2, 64), (9, 500), (4, 512), (3, 520), (1, 2047), (2, 2048), (300, 2056), (700, 4096),
-         (1, 4096), (300, 4097), (270, 8192), (3, 8192), (2, 8200), (2, 16384), (2, 20001), (1, 65536)]
+         (1, 4096), (300, 4097), (5, 6144), (3, 6152), (270, 8192), (3, 8192), (2, 8200), (3, 12288), (2, 12296), (2, 16384), (2, 20001),
+         (1, 65536)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
