@@ -62,47 +62,29 @@ __device__ __forceinline__ void quant_tile_of(int m_tiles, int n_tiles, int& mt,
     nt = __builtin_amdgcn_readfirstlane(in_band / band_rows);
 }
 
-// y from a wave's sums: acc[i][j] holds columns n0 + 16 j .. + 3 of row t0 + 16 i.  Four columns are one store where rows
-// of y keep its alignment.
-template <int MB, int NB>
-__device__ __forceinline__ void quant_store_tile(const QuantLinearArgs& a, int t0, int n0, const i32x4 (&acc)[MB][NB]) {
-    f32x4 sw[NB];
-#pragma unroll
-    for (int j = 0; j < NB; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sw[j][e] = a.w_scale[min(n0 + 16 * j + e, a.cols - 1)];
-    float sx[MB];
-#pragma unroll
-    for (int i = 0; i < MB; ++i) sx[i] = a.x_scale[min(t0 + 16 * i, a.rows - 1)];
+// Four neighbouring columns of y from their sums; sums times the row's scale first, then the columns' ones.
+__device__ __forceinline__ f32x4 quant_scaled(i32x4 v, float sx, f32x4 sw) {
+    return f32x4{static_cast<float>(v[0]), static_cast<float>(v[1]), static_cast<float>(v[2]), static_cast<float>(v[3])} * sx * sw;
+}
+// One store where the rows of y keep its alignment and all four columns exist.
+__device__ __forceinline__ void quant_store4(const QuantLinearArgs& a, int t, int n, f32x4 y) {
     const int size = a.y_type == CATS_F32 ? 4 : 2;
     const bool whole = ((reinterpret_cast<uintptr_t>(a.y) | static_cast<uint64_t>(a.y_ld) * size) & (4 * size - 1)) == 0;
+    char* p = static_cast<char*>(a.y) + (t * a.y_ld + n) * size;
+    const uint2 b = make_uint2(pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3]));
+    if (whole && n + 4 <= a.cols) {
+        if (size == 4)
+            *reinterpret_cast<f32x4*>(p) = y;
+        else
+            *reinterpret_cast<uint2*>(p) = b;
+        return;
+    }
 #pragma unroll
-    for (int i = 0; i < MB; ++i) {
-        const int t = t0 + 16 * i;
-        if (t >= a.rows) return;
-        char* row = static_cast<char*>(a.y) + (t * a.y_ld + n0) * size;
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const int n = n0 + 16 * j;
-            const i32x4 v = acc[i][j];
-            const f32x4 y = f32x4{static_cast<float>(v[0]), static_cast<float>(v[1]), static_cast<float>(v[2]), static_cast<float>(v[3])} * sx[i] * sw[j];
-            const uint2 b = make_uint2(pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3]));
-            char* p = row + 16 * j * size;
-            if (whole && n + 4 <= a.cols) {
-                if (size == 4)
-                    *reinterpret_cast<f32x4*>(p) = y;
-                else
-                    *reinterpret_cast<uint2*>(p) = b;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (n + e >= a.cols) break;
-                    if (size == 4)
-                        reinterpret_cast<float*>(p)[e] = y[e];
-                    else
-                        reinterpret_cast<bf16_t*>(p)[e] = static_cast<bf16_t>((e & 2 ? b.y : b.x) >> 16 * (e & 1));
-                }
-            }
-        }
+    for (int e = 0; e < 4; ++e) {
+        if (n + e >= a.cols) break;
+        if (size == 4)
+            reinterpret_cast<float*>(p)[e] = y[e];
+        else
+            reinterpret_cast<bf16_t*>(p)[e] = static_cast<bf16_t>((e & 2 ? b.y : b.x) >> 16 * (e & 1));
     }
 }

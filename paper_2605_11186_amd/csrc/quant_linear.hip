@@ -26,6 +26,7 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
     constexpr int PB = KW * MB * NB * 1024 <= RING ? MB : MB / 2;
     static_assert(KW * PB * NB * 1024 <= RING && MB % PB == 0, "a part of the sums fits the ring");
     __shared__ __align__(1024) int8_t s_lds[RING];
+    __shared__ __align__(16) float s_sx[16 * MB], s_sw[16 * NB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int mt, nt;
     quant_tile_of(m_tiles, n_tiles, mt, nt);
@@ -34,6 +35,11 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
     const int steps = (a.inner + 127) >> 7;   // (the packed weights may have one step of zeros more)
     const int mine = (steps - wave + KW - 1) / KW;
 
+    // the scales, for when the sums are ready
+    static_assert(MB <= 4 * KW && NB <= 4 * KW, "one of each a thread");
+    const int tid = threadIdx.x;
+    const float sx_own = a.x_scale[min(mt * 16 * MB + min(tid, 16 * MB - 1), a.rows - 1)];
+    const float sw_own = a.w_scale[min(nt * 16 * NB + min(tid, 16 * NB - 1), a.cols - 1)];
     const int piece = ((lane & 7) ^ (lane >> 3)) * 16;   // places of X in LDS: see cats_quant_linear_tiles
     const int8_t* x0 = a.x + static_cast<int64_t>(mt) * 16 * MB * a.x_ld;
     uint32_t xo[2 * MB];
@@ -94,23 +100,24 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
 #pragma unroll
                 for (int j = 0; j < NB; ++j) acc[b][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[h][j], x[h][b], acc[b][j], 0, 0, 0);
     }
-    const int t0 = mt * 16 * MB + r, n0 = nt * 16 * NB + 4 * g;
-    {
-        i32x4* sums = reinterpret_cast<i32x4*>(&s_lds[0]);
+    if (tid < 16 * MB) s_sx[tid] = sx_own;
+    if (tid < 16 * NB) s_sw[tid] = sw_own;
+    i32x4* sums = reinterpret_cast<i32x4*>(&s_lds[0]);
 #pragma unroll
-        for (int b0 = 0; b0 < MB; b0 += PB) {
-            __syncthreads();   // nobody needs its ring, or the part before, any more
+    for (int b0 = 0; b0 < MB; b0 += PB) {
+        __syncthreads();   // nobody needs its ring, or the part before, any more
 #pragma unroll
-            for (int b = 0; b < PB; ++b)
+        for (int b = 0; b < PB; ++b)
 #pragma unroll
-                for (int j = 0; j < NB; ++j) sums[(wave * PB * NB + b * NB + j) * 64 + lane] = acc[b0 + b][j];
-            __syncthreads();
-            for (int f = wave; f < PB * NB; f += KW) {
-                i32x4 one[1][1] = {{sums[f * 64 + lane]}};
+            for (int j = 0; j < NB; ++j) sums[(wave * PB * NB + b * NB + j) * 64 + lane] = acc[b0 + b][j];
+        __syncthreads();
+        for (int f = wave; f < PB * NB; f += KW) {
+            i32x4 sum = sums[f * 64 + lane];
 #pragma unroll
-                for (int q = 1; q < KW; ++q) one[0][0] += sums[(q * PB * NB + f) * 64 + lane];
-                quant_store_tile<1, 1>(a, t0 + 16 * (b0 + f / NB), n0 + 16 * (f % NB), one);
-            }
+            for (int q = 1; q < KW; ++q) sum += sums[(q * PB * NB + f) * 64 + lane];
+            const int t = 16 * (b0 + f / NB) + r, n = 16 * (f % NB) + 4 * g;   // in the tile
+            if (mt * 16 * MB + t < a.rows && nt * 16 * NB + n < a.cols)
+                quant_store4(a, mt * 16 * MB + t, nt * 16 * NB + n, quant_scaled(sum, s_sx[t], *reinterpret_cast<const f32x4*>(s_sw + n)));
         }
     }
 }

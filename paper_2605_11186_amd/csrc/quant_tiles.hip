@@ -17,6 +17,7 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
     static_assert(MB % NB == 0 && 2 * MB % COPIES == 0, "requests dealt evenly");
     static_assert(COPIES * 8 * WAVES == BM, "rows dealt evenly");
     __shared__ __align__(1024) int8_t s_x[NS][BM * 128];
+    __shared__ __align__(16) float s_sx[BM], s_sw[BN];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
@@ -25,6 +26,11 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
     const int steps = a.chunks >> 1;
     const int k_last = (a.inner - 1) / 16 * 16;
     const int n_rb = (a.cols + QPACK_ROWS - 1) / QPACK_ROWS;
+    // the scales, for when the sums are ready
+    static_assert(BM <= 64 * WAVES && BN <= 64 * WAVES, "one of each a thread");
+    const int tid = threadIdx.x;
+    const float sx_own = a.x_scale[min(mt * BM + min(tid, BM - 1), a.rows - 1)];
+    const float sw_own = a.w_scale[min(nt * BN + min(tid, BN - 1), a.cols - 1)];
     // X: lane l copies piece (l % 8) ^ (l / 8) of row l / 8 of its eight rows: piece p of row r lies at place p ^ (r % 8) of
     // the row's 128 bytes, so that the eight lanes that read neighbouring rows at once find different banks
     const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
@@ -96,15 +102,24 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
     };
-#pragma unroll
-    for (int s = 0; s < NS - 1; ++s)
-#pragma unroll
-        for (int i = 0; i < COPIES; ++i) copy_piece(s, s, i);
-#pragma unroll
-    for (int c = 0; c < WS - 1; ++c)
+    // What the first step needs comes first: X of step 0, W of its chunks, X of step 1.
+    auto load_chunk = [&](int c) {
 #pragma unroll
         for (int j = 0; j < NB; ++j) w[c][j] = load_w(c, j);
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((WS - 1) * NB) : "memory");
+    };
+    static_assert(NS == 4 && WS == 4, "order and counts of the first requests");
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) copy_piece(0, 0, i);
+    load_chunk(0);
+    load_chunk(1);
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) copy_piece(1, 1, i);
+    load_chunk(2);
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) copy_piece(2, 2, i);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES + NB) : "memory");
+    if (tid < BM) s_sx[tid] = sx_own;
+    if (tid < BN) s_sw[tid] = sw_own;
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
@@ -116,8 +131,45 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
         step(s + 1, slot, std::integral_constant<int, 1>{});
         slot = next_slot(slot);
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy may land after the workgroup's end
-    quant_store_tile<MB, NB>(a, mt * BM + wm * MB * 16 + r, nt * BN + wn * NB * 16 + 4 * g, acc);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy may land after the workgroup's end, nor where y passes now
+    __syncthreads();
+    // Four columns a lane are short runs of a row in bf16: a row block goes through LDS (each wave has its own place) and leaves as
+    // eight columns a lane, whole lines of y.  With the scales
+    // read ahead: 4096 x 4096 x 256 16.6 -> 12.7 us.
+    constexpr int ROW = 16 * NB * 2 + 16;   // bytes of a row there: data and 16, so that rows start at different banks
+    static_assert(WAVES * 16 * ROW <= NS * BM * 128, "a place for each wave");
+    int8_t* mine = &s_x[0][0] + wave * 16 * ROW;
+    const bool wide = a.y_type == CATS_BF16 && ((reinterpret_cast<uintptr_t>(a.y) | static_cast<uint64_t>(a.y_ld) * 2) & 15) == 0 &&
+                      nt * BN + BN <= a.cols;
+    const float* swp = s_sw + wn * NB * 16 + 4 * g;
+    f32x4 sw[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) sw[j] = *reinterpret_cast<const f32x4*>(swp + 16 * j);
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+        const float sx = s_sx[(wm * MB + i) * 16 + r];
+        f32x4 y[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) y[j] = quant_scaled(acc[i][j], sx, sw[j]);
+        const int t = mt * BM + (wm * MB + i) * 16, n = nt * BN + wn * NB * 16;
+        if (wide) {
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                *reinterpret_cast<uint2*>(mine + r * ROW + 32 * j + 8 * g) = make_uint2(pack_bf2(y[j][0], y[j][1]), pack_bf2(y[j][2], y[j][3]));
+            __builtin_amdgcn_wave_barrier();
+            constexpr int LANES = 2 * NB;   // of a row
+#pragma unroll
+            for (int k = 0; k < 16 * LANES / 64; ++k) {
+                const int row = k * (64 / LANES) + lane / LANES, at16 = lane % LANES;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * ROW + at16 * 16);
+                if (t + row < a.rows) *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.y) + (t + row) * a.y_ld + n + at16 * 8) = v;
+            }
+            __builtin_amdgcn_wave_barrier();
+        } else if (t + r < a.rows) {
+#pragma unroll
+            for (int j = 0; j < NB; ++j) quant_store4(a, t + r, n + 16 * j + 4 * g, y[j]);
+        }
+    }
 }
 
 template <int WM, int WN, int MB, int NB, int NS, int WS>
