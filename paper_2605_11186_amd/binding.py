@@ -374,109 +374,109 @@ def cats_lm_head_argmax(ctx, hidden, g_final, w_lm, argmax_out, logits_out=None,
                                          _dp(logits_out), _dp(argmax_out), _dp(margin_out), _stream(stream)))
 
 
-class _Types:
-    """torch's types that the operators take (filled in by their first call: importing this module does not import torch)."""
-    f32 = bf16 = i8 = current_device = None
-    code = {}
-
-    @classmethod
-    def load(cls):
-        import torch
-        cls.f32, cls.bf16, cls.i8 = torch.float32, torch.bfloat16, torch.int8
-        cls.current_device = staticmethod(torch.cuda.current_device)
-        cls.code = {torch.float32: CATS_F32, torch.bfloat16: CATS_BF16}
+# torch's types that the operators in 8 bits take, filled in by their first call (importing this module does not import torch)
+_f32 = _bf16 = _i8 = _current_device = None
+_code_of = {}
 
 
-def _device_and_code(t):
-    """Device number of a tensor (-1: host memory) and CATS_F32, CATS_BF16 or None for its type."""
-    if not _Types.code:
-        _Types.load()
-    return t.get_device(), _Types.code.get(t.dtype)
+def _load_types():
+    global _f32, _bf16, _i8, _current_device
+    import torch
+    _f32, _bf16, _i8, _current_device = torch.float32, torch.bfloat16, torch.int8, torch.cuda.current_device
+    _code_of.update({_f32: CATS_F32, _bf16: CATS_BF16})
 
 
-def _unfit(name, t, dtype, shape, device):
-    return CatsError(CATS_EINVAL, f"{name}: {dtype} {list(shape)} with neighbouring elements on device {device} expected, got "
-                                  f"{t.dtype} {list(t.shape)}, strides {list(t.stride())} on device {t.get_device()}")
+# A small call is mostly host time, so the operators check their operands in place, in the cheapest terms, and leave it to
+# these to say what was wrong.
+def _refuse_operands(device, **operands):
+    """operands: name = (tensor, type or types, shape).  Rows have to lie in one piece each, vectors to be contiguous."""
+    for name, (t, types, shape) in operands.items():
+        types = types if isinstance(types, tuple) else (types,)
+        if (t.dtype not in types or tuple(t.shape) != shape or t.get_device() != device or
+                (len(shape) == 1 and not t.is_contiguous()) or (shape[-1] > 1 and t.stride(-1) != 1)):
+            raise CatsError(CATS_EINVAL, f"{name}: {' or '.join(map(str, types))} {list(shape)} with neighbouring elements on device "
+                                         f"{device} expected, got {t.dtype} {list(t.shape)}, strides {list(t.stride())} on device "
+                                         f"{t.get_device()}")
+    raise CatsError(CATS_EINVAL, f"tensors on device {device}, which is not the current GPU")
 
 
-def _rows_of(name, t, dtype, rows, cols, device):
-    """Checks of a [rows][cols] operand whose rows lie in one piece each; returns its row stride in elements."""
-    if t.dtype is not dtype or t.shape != (rows, cols) or t.get_device() != device:
-        raise _unfit(name, t, dtype, (rows, cols), device)
-    ld, step = t.stride()
-    if step != 1 and cols > 1:
-        raise _unfit(name, t, dtype, (rows, cols), device)
-    # the stride of a single row says nothing: any that suits a row of this length will do
-    return ld if rows > 1 else (cols + 15) // 16 * 16
-
-
-def _vector(name, t, dtype, n, device):
-    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
-        raise _unfit(name, t, dtype, (n,), device)
-    return t.data_ptr()
-
-
-def _current(device, stream):
-    """The operators run on the current device: refuse tensors and streams that belong elsewhere.  Returns the stream's handle."""
-    if device < 0 or device != _Types.current_device():
-        raise CatsError(CATS_EINVAL, f"tensors on device {device}, which is not the current GPU")
-    if stream is None:
-        return None
-    if getattr(stream, "device_index", device) != device:
+def _stream_on(device, stream):
+    """A stream's handle; a torch stream has to belong to the tensors' device."""
+    if stream is not None and getattr(stream, "device_index", device) != device:
         raise CatsError(CATS_EINVAL, f"stream of device {stream.device_index}, tensors on device {device}")
-    return getattr(stream, "cuda_stream", stream)
+    return _stream(stream)
 
 
-def _floats(name, code, t):
-    if code is None:
-        raise CatsError(CATS_EINVAL, f"{name}: float32 or bfloat16 expected, got {t.dtype}")
-    return code
+def _row_stride(stride, rows, cols):
+    # the stride of a single row says nothing: any that suits a row of this length will do
+    return stride if rows > 1 else (cols + 15) // 16 * 16
 
 
 def cats_quantize_rows(src, q_out, scale_out, stream=None):
     """Rows of src (float32 or bfloat16 [rows][cols]) as int8 with one float32 scale each."""
-    rows, cols = src.shape
-    dev, code = _device_and_code(src)
-    code, ld = _floats("src", code, src), _rows_of("src", src, src.dtype, rows, cols, dev)
-    q_ld = _rows_of("q_out", q_out, _Types.i8, rows, cols, dev)
-    scale = _vector("scale_out", scale_out, _Types.f32, rows, dev)
-    st = _current(dev, stream)
+    if _f32 is None:
+        _load_types()
+    rows, cols = shape = src.shape
+    dev, code = src.get_device(), _code_of.get(src.dtype)
+    (ld, step), (q_ld, q_step) = src.stride(), q_out.stride()
+    if (code is None or q_out.dtype is not _i8 or scale_out.dtype is not _f32 or q_out.shape != shape or scale_out.shape != (rows,) or
+            (cols > 1 and (step != 1 or q_step != 1)) or not scale_out.is_contiguous() or q_out.get_device() != dev or
+            scale_out.get_device() != dev or dev < 0 or dev != _current_device()):
+        _refuse_operands(dev, src=(src, (_f32, _bf16), (rows, cols)), q_out=(q_out, _i8, (rows, cols)),
+                         scale_out=(scale_out, _f32, (rows,)))
     if rows:
-        _check(library().cats_quantize_rows(src.data_ptr(), code, ld, rows, cols, q_out.data_ptr(), q_ld, scale, st))
+        _check(library().cats_quantize_rows(src.data_ptr(), code, _row_stride(ld, rows, cols), rows, cols, q_out.data_ptr(),
+                                                 _row_stride(q_ld, rows, cols), scale_out.data_ptr(), _stream_on(dev, stream)))
 
 
 def cats_rmsnorm_quantize(x, gain, eps: float, q_out, scale_out, delta=None, x_out=None, stream=None):
     """x (float32 [rows][cols]) plus delta, normalised, times gain, as int8 rows with scales.  With delta the sum
     goes to x_out, or back to x if none is given."""
-    rows, cols = x.shape
-    dev, _ = _device_and_code(x)
-    ld = _rows_of("x", x, _Types.f32, rows, cols, dev)
-    g = _vector("gain", gain, _Types.bf16, cols, dev)
-    q_ld = _rows_of("q_out", q_out, _Types.i8, rows, cols, dev)
-    scale = _vector("scale_out", scale_out, _Types.f32, rows, dev)
-    d_ptr, d_code, d_ld, o_ptr, o_ld = None, 0, 0, None, 0
+    if _f32 is None:
+        _load_types()
+    rows, cols = shape = x.shape
+    dev = x.get_device()
+    (ld, step), (q_ld, q_step) = x.stride(), q_out.stride()
+    d_ptr, d_code, d_ld, o_ptr, o_ld, ok = None, 0, 0, None, 0, True
     if delta is not None:
-        d_code, d_ld = _floats("delta", _Types.code.get(delta.dtype), delta), _rows_of("delta", delta, delta.dtype, rows, cols, dev)
         out = x if x_out is None else x_out
-        d_ptr, o_ptr, o_ld = delta.data_ptr(), out.data_ptr(), _rows_of("x_out", out, _Types.f32, rows, cols, dev)
+        (d_ld, d_step), (o_ld, o_step) = delta.stride(), out.stride()
+        d_code, d_ptr, o_ptr = _code_of.get(delta.dtype), delta.data_ptr(), out.data_ptr()
+        d_ld, o_ld = _row_stride(d_ld, rows, cols), _row_stride(o_ld, rows, cols)
+        ok = (d_code is not None and delta.shape == shape and out.shape == shape and out.dtype is _f32 and
+              (cols == 1 or d_step == o_step == 1) and delta.get_device() == dev and out.get_device() == dev)
     elif x_out is not None:
         raise CatsError(CATS_EINVAL, "x_out without delta: x does not change")
-    st = _current(dev, stream)
+    if (not ok or x.dtype is not _f32 or gain.dtype is not _bf16 or q_out.dtype is not _i8 or scale_out.dtype is not _f32 or
+            q_out.shape != shape or gain.shape != (cols,) or scale_out.shape != (rows,) or
+            (cols > 1 and (step != 1 or q_step != 1)) or not gain.is_contiguous() or not scale_out.is_contiguous() or
+            q_out.get_device() != dev or gain.get_device() != dev or scale_out.get_device() != dev or dev < 0 or
+            dev != _current_device()):
+        more = {} if delta is None else dict(delta=(delta, (_f32, _bf16), (rows, cols)), x_out=(out, _f32, (rows, cols)))
+        _refuse_operands(dev, x=(x, _f32, (rows, cols)), gain=(gain, _bf16, (cols,)), q_out=(q_out, _i8, (rows, cols)),
+                         scale_out=(scale_out, _f32, (rows,)), **more)
     if rows:
-        _check(library().cats_rmsnorm_quantize(x.data_ptr(), ld, d_ptr, d_code, d_ld, g, eps, rows, cols, o_ptr, o_ld,
-                                               q_out.data_ptr(), q_ld, scale, st))
+        _check(library().cats_rmsnorm_quantize(x.data_ptr(), _row_stride(ld, rows, cols), d_ptr, d_code, d_ld, gain.data_ptr(),
+                                                    eps, rows, cols, o_ptr, o_ld, q_out.data_ptr(), _row_stride(q_ld, rows, cols),
+                                                    scale_out.data_ptr(), _stream_on(dev, stream)))
 
 
 def cats_swiglu_quantize(gate_up, q_out, scale_out, stream=None):
     """silu(gate) * up of gate_up (float32 or bfloat16 [rows][2 cols], gate | up) as int8 rows with scales."""
+    if _f32 is None:
+        _load_types()
     rows, cols = q_out.shape
-    dev, code = _device_and_code(gate_up)
-    code, ld = _floats("gate_up", code, gate_up), _rows_of("gate_up", gate_up, gate_up.dtype, rows, 2 * cols, dev)
-    q_ld = _rows_of("q_out", q_out, _Types.i8, rows, cols, dev)
-    scale = _vector("scale_out", scale_out, _Types.f32, rows, dev)
-    st = _current(dev, stream)
+    dev, code = gate_up.get_device(), _code_of.get(gate_up.dtype)
+    (ld, step), (q_ld, q_step) = gate_up.stride(), q_out.stride()
+    if (code is None or q_out.dtype is not _i8 or scale_out.dtype is not _f32 or gate_up.shape != (rows, 2 * cols) or
+            scale_out.shape != (rows,) or step != 1 or (cols > 1 and q_step != 1) or not scale_out.is_contiguous() or
+            q_out.get_device() != dev or scale_out.get_device() != dev or dev < 0 or dev != _current_device()):
+        _refuse_operands(dev, gate_up=(gate_up, (_f32, _bf16), (rows, 2 * cols)), q_out=(q_out, _i8, (rows, cols)),
+                         scale_out=(scale_out, _f32, (rows,)))
     if rows:
-        _check(library().cats_swiglu_quantize(gate_up.data_ptr(), code, ld, rows, cols, q_out.data_ptr(), q_ld, scale, st))
+        _check(library().cats_swiglu_quantize(gate_up.data_ptr(), code, _row_stride(ld, rows, 2 * cols), rows, cols,
+                                                   q_out.data_ptr(), _row_stride(q_ld, rows, cols), scale_out.data_ptr(),
+                                                   _stream_on(dev, stream)))
 
 
 def cats_packed_quantized_bytes(rows: int, cols: int) -> int:
@@ -486,28 +486,40 @@ def cats_packed_quantized_bytes(rows: int, cols: int) -> int:
 def cats_pack_quantized_matrix(src, stream=None):
     """Packed copy of int8 weights [out][in] (new device tensor, int8)."""
     import torch
+    if _f32 is None:
+        _load_types()
     rows, cols = src.shape
-    dev, _ = _device_and_code(src)
-    ld = _rows_of("src", src, torch.int8, rows, cols, dev)
-    st = _current(dev, stream)
+    dev, (ld, step) = src.get_device(), src.stride()
+    if src.dtype is not _i8 or (cols > 1 and step != 1) or dev < 0 or dev != _current_device():
+        _refuse_operands(dev, src=(src, _i8, (rows, cols)))
     dst = torch.empty(cats_packed_quantized_bytes(rows, cols), dtype=torch.int8, device=src.device)
-    _check(library().cats_pack_quantized_matrix(src.data_ptr(), ld, rows, cols, dst.data_ptr(), st))
+    _check(library().cats_pack_quantized_matrix(src.data_ptr(), _row_stride(ld, rows, cols), rows, cols, dst.data_ptr(),
+                                                _stream_on(dev, stream)))
     return dst
 
 
 def cats_quantized_linear(x, x_scale, w_packed, w_scale, out, stream=None):
     """out [rows][cols] (float32 or bfloat16) = (x . W) * x_scale * w_scale for int8 x [rows][inner] and packed int8 W [cols][inner]."""
-    (rows, inner), (_, cols) = x.shape, out.shape
-    dev, code = _device_and_code(out)
-    code, ld = _floats("out", code, out), _rows_of("x", x, _Types.i8, rows, inner, dev)
-    y_ld = _rows_of("out", out, out.dtype, rows, cols, dev)
-    sx, sw = _vector("x_scale", x_scale, _Types.f32, rows, dev), _vector("w_scale", w_scale, _Types.f32, cols, dev)
-    w = _vector("w_packed", w_packed, _Types.i8, (cols + 15) // 16 * ((inner + 255) // 256) * 4096, dev)
+    if _f32 is None:
+        _load_types()
+    (rows, inner), (out_rows, cols) = x.shape, out.shape
+    dev, code = x.get_device(), _code_of.get(out.dtype)
+    (ld, step), (y_ld, y_step) = x.stride(), out.stride()
+    packed = (cols + 15) // 16 * ((inner + 255) // 256) * 4096
+    if (code is None or x.dtype is not _i8 or w_packed.dtype is not _i8 or x_scale.dtype is not _f32 or w_scale.dtype is not _f32 or
+            out_rows != rows or x_scale.shape != (rows,) or w_scale.shape != (cols,) or w_packed.shape != (packed,) or
+            (inner > 1 and step != 1) or (cols > 1 and y_step != 1) or not x_scale.is_contiguous() or not w_scale.is_contiguous() or
+            not w_packed.is_contiguous() or out.get_device() != dev or x_scale.get_device() != dev or w_scale.get_device() != dev or
+            w_packed.get_device() != dev or dev < 0 or dev != _current_device()):
+        _refuse_operands(dev, x=(x, _i8, (rows, inner)), x_scale=(x_scale, _f32, (rows,)), w_packed=(w_packed, _i8, (packed,)),
+                         w_scale=(w_scale, _f32, (cols,)), out=(out, (_f32, _bf16), (rows, cols)))
+    ld = _row_stride(ld, rows, inner)
     if inner % 16 and x.untyped_storage().nbytes() < x.storage_offset() + (rows - 1) * ld + (inner + 15) // 16 * 16:
         raise CatsError(CATS_EINVAL, "x: its last row must be readable up to a multiple of 16 bytes")
-    st = _current(dev, stream)
     if rows:
-        _check(library().cats_quantized_linear(x.data_ptr(), ld, sx, w, sw, out.data_ptr(), code, y_ld, rows, cols, inner, st))
+        _check(library().cats_quantized_linear(x.data_ptr(), ld, x_scale.data_ptr(), w_packed.data_ptr(), w_scale.data_ptr(),
+                                                    out.data_ptr(), code, _row_stride(y_ld, rows, cols), rows, cols, inner,
+                                                    _stream_on(dev, stream)))
 
 
 def quantize_layer(tensors: dict) -> dict:
