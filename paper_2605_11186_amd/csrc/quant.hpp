@@ -41,8 +41,8 @@ struct QuantLinearArgs {
     int y_type;
 };
 void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st);
-void launch_quant_tiles(const QuantLinearArgs& a, hipStream_t st);        // tiles of 256 x 256
-void launch_quant_tiles_half(const QuantLinearArgs& a, hipStream_t st);   // of 128 rows x 256 columns
+void launch_quant_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st);        // tiles of 256 x 256
+void launch_quant_tiles_half(const QuantLinearArgs& a, int n_cus, hipStream_t st);   // of 128 rows x 256 columns
 
 // 64 lanes copy 16 bytes each from base + their own offset to 1024 consecutive bytes of LDS (at byte `lds`), with no
 // register between.  Counted in vmcnt like a load; the compiler does not see it and waits for nothing on its account.
@@ -50,12 +50,12 @@ __device__ __forceinline__ void copy_to_lds(const int8_t* base, uint32_t offset,
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
 
-// The tile of this workgroup.  Workgroup b runs on XCD b % 8: an XCD takes a run of tiles, in bands of 4 row tiles (a run of
-// tiles of one band shares rows of X and of W in the XCD's L2).
-__device__ __forceinline__ void quant_tile_of(int m_tiles, int n_tiles, int& mt, int& nt) {
+// Tile number `index` (of a launch's workgroups).  Workgroup b runs on XCD b % 8: an XCD takes a run of tiles, in bands of 4 row
+// tiles (a run of tiles of one band shares rows of X and of W in the XCD's L2).
+__device__ __forceinline__ void quant_tile_of(int index, int m_tiles, int n_tiles, int& mt, int& nt) {
     constexpr int BAND = 4;
-    const int total = m_tiles * n_tiles, xcd = blockIdx.x & 7;
-    const int id = xcd * (total >> 3) + min(xcd, total & 7) + (blockIdx.x >> 3);
+    const int total = m_tiles * n_tiles, xcd = index & 7;
+    const int id = xcd * (total >> 3) + min(xcd, total & 7) + (index >> 3);
     const int band = id / (BAND * n_tiles), in_band = id - band * BAND * n_tiles;
     const int band_rows = min(BAND, m_tiles - band * BAND);
     mt = __builtin_amdgcn_readfirstlane(band * BAND + in_band % band_rows);

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
     __shared__ __align__(16) float s_sx[16 * MB], s_sw[16 * NB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int mt, nt;
-    quant_tile_of(m_tiles, n_tiles, mt, nt);
+    quant_tile_of(blockIdx.x, m_tiles, n_tiles, mt, nt);
     const int n_rb = (a.cols + QPACK_ROWS - 1) / QPACK_ROWS;
     const int k_last = (a.inner - 1) / 16 * 16;
     const int steps = (a.inner + 127) >> 7;   // (the packed weights may have one step of zeros more)
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
 }
 
 template <int MB, int NB, int KW, int NS>
-void launch_split(const QuantLinearArgs& a, hipStream_t st) {
+void launch_split(const QuantLinearArgs& a, int, hipStream_t st) {
     const int m_tiles = (a.rows + 16 * MB - 1) / (16 * MB), n_tiles = (a.cols + 16 * NB - 1) / (16 * NB);
     hipLaunchKernelGGL((cats_quant_linear_split<MB, NB, KW, NS>), dim3(static_cast<unsigned>(m_tiles) * n_tiles), dim3(64 * KW), 0,
                        st, a, m_tiles, n_tiles);
@@ -170,12 +170,12 @@ int quant_cus() {
 
 void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
     if (a.rows < 1) return;
-    static constexpr void (*LAUNCH[])(const QuantLinearArgs&, hipStream_t) = {
+    static constexpr void (*LAUNCH[])(const QuantLinearArgs&, int, hipStream_t) = {
         launch_split<1, 1, 8, 1>, launch_split<1, 2, 8, 1>, launch_split<2, 2, 8, 1>, launch_split<4, 2, 4, 2>, launch_split<4, 3, 4, 1>,
         launch_split<4, 4, 4, 1>, launch_split<4, 6, 4, 1>, launch_split<6, 6, 4, 1>, launch_split<8, 4, 4, 1>, launch_split<8, 6, 4, 1>,
         launch_split<8, 8, 4, 1>, launch_quant_tiles_half,  launch_quant_tiles};
     static_assert(sizeof(LAUNCH) / sizeof(LAUNCH[0]) == N_QUANT_TILES, "one kernel for each tile");
-    LAUNCH[quant_tile_choice(a.rows, a.cols, n_cus)](a, st);
+    LAUNCH[quant_tile_choice(a.rows, a.cols, n_cus)](a, n_cus, st);
 }
 
 extern "C" {

@@ -16,54 +16,70 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
     static_assert(4 % WS == 0, "places of W come round again after a pair of steps");
     static_assert(MB % NB == 0 && 2 * MB % COPIES == 0, "requests dealt evenly");
     static_assert(COPIES * 8 * WAVES == BM, "rows dealt evenly");
+    constexpr int ROW = 16 * NB * 2 + 16;   // bytes of a row of y on its way out: data and 16, so that rows start at different banks
     __shared__ __align__(1024) int8_t s_x[NS][BM * 128];
-    __shared__ __align__(16) float s_sx[BM], s_sw[BN];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ __align__(16) int8_t s_y[WAVES][16 * ROW];
+    __shared__ __align__(16) float s_sx[2][BM], s_sw[2][BN];   // by parity of the tile
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
-
-    int mt, nt;
-    quant_tile_of(m_tiles, n_tiles, mt, nt);
     const int steps = a.chunks >> 1;
     const int k_last = (a.inner - 1) / 16 * 16;
     const int n_rb = (a.cols + QPACK_ROWS - 1) / QPACK_ROWS;
-    // the scales, for when the sums are ready
-    static_assert(BM <= 64 * WAVES && BN <= 64 * WAVES, "one of each a thread");
-    const int tid = threadIdx.x;
-    const float sx_own = a.x_scale[min(mt * BM + min(tid, BM - 1), a.rows - 1)];
-    const float sw_own = a.w_scale[min(nt * BN + min(tid, BN - 1), a.cols - 1)];
+
+    // ---- the tile whose operands are requested
+    int mt, nt;
     // X: lane l copies piece (l % 8) ^ (l / 8) of row l / 8 of its eight rows: piece p of row r lies at place p ^ (r % 8) of
     // the row's 128 bytes, so that the eight lanes that read neighbouring rows at once find different banks
     const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
-    const int8_t* x0 = a.x + static_cast<int64_t>(mt) * BM * a.x_ld;
-    uint32_t xo[COPIES];   // the launcher sees to it that a tile of X spans less than 2^31 bytes
-#pragma unroll
-    for (int i = 0; i < COPIES; ++i)
-        xo[i] = min((wave * COPIES + i) * 8 + (lane >> 3), a.rows - 1 - mt * BM) * static_cast<int>(a.x_ld);
+    const int8_t* x0;
+    uint32_t xo[COPIES];   // (a tile of X spans less than 2^31 bytes: CATS_QUANT_MAX_LD)
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&s_x[0][0])) + wave * COPIES * 1024;
     auto copy_piece = [&](int s, int slot, int i) {
         // past the end of a row of X the weights are zeros: any value will do there
         copy_to_lds(x0, xo[i] + min(s * 128 + piece, k_last), lds0 + slot * (BM * 128) + i * 1024);
     };
-    // W
-    // (row blocks and chunks that do not exist are read from the last ones: their products are not stored, or not made)
-    const int rb0 = min(nt * (BN / 16) + wn * NB, n_rb - 1);
-    const int w_bytes = __builtin_amdgcn_readfirstlane(min(NB, n_rb - rb0) * a.chunks * QPACK_FRAG);
-    const __amdgpu_buffer_rsrc_t w_buf = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<int8_t*>(a.w + static_cast<int64_t>(rb0) * a.chunks * QPACK_FRAG), 0, w_bytes, 0x00020000);
+    // W (row blocks and chunks that do not exist are read from the last ones: their products are not stored, or not made)
+    __amdgpu_buffer_rsrc_t w_buf;
     int w_at[NB];
-#pragma unroll
-    for (int j = 0; j < NB; ++j) w_at[j] = __builtin_amdgcn_readfirstlane(min(j, n_rb - 1 - rb0) * a.chunks * QPACK_FRAG);
-    const int wo = lane * 16;
     i32x4 w[WS][NB];   // chunk c in place c % WS, WS - 1 chunks ahead
     auto load_w = [&](int c, int j) {
-        return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_buf, wo, w_at[j] + min(c, a.chunks - 1) * QPACK_FRAG, 0));
+        return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(w_buf, lane * 16, w_at[j] + min(c, a.chunks - 1) * QPACK_FRAG, 0));
     };
-    i32x4 acc[MB][NB];
+    // the scales, for when the sums are ready
+    static_assert(BM <= 64 * WAVES && BN <= 64 * WAVES, "one of each a thread");
+    float sx_own, sw_own;
+    auto enter = [&](int index) {
+        quant_tile_of(index, m_tiles, n_tiles, mt, nt);
+        sx_own = a.x_scale[min(mt * BM + min(tid, BM - 1), a.rows - 1)];
+        sw_own = a.w_scale[min(nt * BN + min(tid, BN - 1), a.cols - 1)];
+        x0 = a.x + static_cast<int64_t>(mt) * BM * a.x_ld;
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+        for (int i = 0; i < COPIES; ++i)
+            xo[i] = min((wave * COPIES + i) * 8 + (lane >> 3), a.rows - 1 - mt * BM) * static_cast<int>(a.x_ld);
+        const int rb0 = min(nt * (BN / 16) + wn * NB, n_rb - 1);
+        const int w_bytes = __builtin_amdgcn_readfirstlane(min(NB, n_rb - rb0) * a.chunks * QPACK_FRAG);
+        w_buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(a.w + static_cast<int64_t>(rb0) * a.chunks * QPACK_FRAG), 0,
+                                                  w_bytes, 0x00020000);
 #pragma unroll
-        for (int j = 0; j < NB; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+        for (int j = 0; j < NB; ++j) w_at[j] = __builtin_amdgcn_readfirstlane(min(j, n_rb - 1 - rb0) * a.chunks * QPACK_FRAG);
+        // What the first step needs comes first: X of step 0, W of its chunks, X of step 1.
+        auto load_chunk = [&](int c) {
+#pragma unroll
+            for (int j = 0; j < NB; ++j) w[c][j] = load_w(c, j);
+        };
+        static_assert(NS == 4 && WS == 4, "order and counts of the first requests");
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) copy_piece(0, 0, i);
+        load_chunk(0);
+        load_chunk(1);
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) copy_piece(1, 1, i);
+        load_chunk(2);
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) copy_piece(2, 2, i);
+    };
 
+    i32x4 acc[MB][NB];
     const int r = lane & 15, g = lane >> 4;
     const int8_t* xs = &s_x[0][0] + (wm * MB * 16 + r) * 128;
     // fragment f of a step: block f % MB of rows, chunk f / MB
@@ -102,85 +118,80 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
     };
-    // What the first step needs comes first: X of step 0, W of its chunks, X of step 1.
-    auto load_chunk = [&](int c) {
+    enter(blockIdx.x);
+    const int total = m_tiles * n_tiles;
+    for (int index = blockIdx.x, parity = 0;; parity ^= 1) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES + NB) : "memory");
+        if (tid < BM) s_sx[parity][tid] = sx_own;
+        if (tid < BN) s_sw[parity][tid] = sw_own;
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
 #pragma unroll
-        for (int j = 0; j < NB; ++j) w[c][j] = load_w(c, j);
-    };
-    static_assert(NS == 4 && WS == 4, "order and counts of the first requests");
+        for (int i = 0; i < MB; ++i)
 #pragma unroll
-    for (int i = 0; i < COPIES; ++i) copy_piece(0, 0, i);
-    load_chunk(0);
-    load_chunk(1);
+            for (int j = 0; j < NB; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < COPIES; ++i) copy_piece(1, 1, i);
-    load_chunk(2);
-#pragma unroll
-    for (int i = 0; i < COPIES; ++i) copy_piece(2, 2, i);
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES + NB) : "memory");
-    if (tid < BM) s_sx[tid] = sx_own;
-    if (tid < BN) s_sw[tid] = sw_own;
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int f = 0; f < AHEAD; ++f) x[f] = read_x(0, f);
-    int slot = 0, s = 0;
-    for (; s < steps; s += 2) {   // packed weights end with a whole pair of steps
-        step(s, slot, std::integral_constant<int, 0>{});
-        slot = next_slot(slot);
-        step(s + 1, slot, std::integral_constant<int, 1>{});
-        slot = next_slot(slot);
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy may land after the workgroup's end, nor where y passes now
-    __syncthreads();
-    // Four columns a lane are short runs of a row in bf16: a row block goes through LDS (each wave has its own place) and leaves as
-    // eight columns a lane, whole lines of y.  With the scales
-    // read ahead: 4096 x 4096 x 256 16.6 -> 12.7 us.
-    constexpr int ROW = 16 * NB * 2 + 16;   // bytes of a row there: data and 16, so that rows start at different banks
-    static_assert(WAVES * 16 * ROW <= NS * BM * 128, "a place for each wave");
-    int8_t* mine = &s_x[0][0] + wave * 16 * ROW;
-    const bool wide = a.y_type == CATS_BF16 && ((reinterpret_cast<uintptr_t>(a.y) | static_cast<uint64_t>(a.y_ld) * 2) & 15) == 0 &&
-                      nt * BN + BN <= a.cols;
-    const float* swp = s_sw + wn * NB * 16 + 4 * g;
-    f32x4 sw[NB];
-#pragma unroll
-    for (int j = 0; j < NB; ++j) sw[j] = *reinterpret_cast<const f32x4*>(swp + 16 * j);
-#pragma unroll
-    for (int i = 0; i < MB; ++i) {
-        const float sx = s_sx[(wm * MB + i) * 16 + r];
-        f32x4 y[NB];
-#pragma unroll
-        for (int j = 0; j < NB; ++j) y[j] = quant_scaled(acc[i][j], sx, sw[j]);
-        const int t = mt * BM + (wm * MB + i) * 16, n = nt * BN + wn * NB * 16;
-        if (wide) {
-#pragma unroll
-            for (int j = 0; j < NB; ++j)
-                *reinterpret_cast<uint2*>(mine + r * ROW + 32 * j + 8 * g) = make_uint2(pack_bf2(y[j][0], y[j][1]), pack_bf2(y[j][2], y[j][3]));
-            __builtin_amdgcn_wave_barrier();
-            constexpr int LANES = 2 * NB;   // of a row
-#pragma unroll
-            for (int k = 0; k < 16 * LANES / 64; ++k) {
-                const int row = k * (64 / LANES) + lane / LANES, at16 = lane % LANES;
-                const u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * ROW + at16 * 16);
-                if (t + row < a.rows) *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.y) + (t + row) * a.y_ld + n + at16 * 8) = v;
-            }
-            __builtin_amdgcn_wave_barrier();
-        } else if (t + r < a.rows) {
-#pragma unroll
-            for (int j = 0; j < NB; ++j) quant_store4(a, t + r, n + 16 * j + 4 * g, y[j]);
+        for (int f = 0; f < AHEAD; ++f) x[f] = read_x(0, f);
+        int slot = 0;
+        for (int s = 0; s < steps; s += 2) {   // packed weights end with a whole pair of steps
+            step(s, slot, std::integral_constant<int, 0>{});
+            slot = next_slot(slot);
+            step(s + 1, slot, std::integral_constant<int, 1>{});
+            slot = next_slot(slot);
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy may land after the workgroup's end, or in the next tile's X
+        __syncthreads();
+        // the next tile's operands come while this one's y leaves
+        const int t0 = mt * BM + wm * MB * 16, n0 = nt * BN + wn * NB * 16;
+        const bool inside = nt * BN + BN <= a.cols;
+        index += gridDim.x;
+        const bool more = index < total;
+        if (more) enter(index);
+        // Four columns a lane are short runs of a row in bf16: a row block goes through LDS (each wave has its own place) and leaves
+        // as eight columns a lane, whole lines of y.  With the scales read ahead: 4096 x 4096 x 256 16.6 -> 12.7 us.
+        int8_t* mine = &s_y[wave][0];
+        const bool wide = a.y_type == CATS_BF16 && ((reinterpret_cast<uintptr_t>(a.y) | static_cast<uint64_t>(a.y_ld) * 2) & 15) == 0 && inside;
+        f32x4 sw[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) sw[j] = *reinterpret_cast<const f32x4*>(&s_sw[parity][wn * NB * 16 + 16 * j + 4 * g]);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+            const float sx = s_sx[parity][(wm * MB + i) * 16 + r];
+            const int t = t0 + 16 * i;
+            f32x4 y[NB];
+#pragma unroll
+            for (int j = 0; j < NB; ++j) y[j] = quant_scaled(acc[i][j], sx, sw[j]);
+            if (wide) {
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                    *reinterpret_cast<uint2*>(mine + r * ROW + 32 * j + 8 * g) = make_uint2(pack_bf2(y[j][0], y[j][1]), pack_bf2(y[j][2], y[j][3]));
+                __builtin_amdgcn_wave_barrier();
+                constexpr int LANES = 2 * NB;   // of a row
+#pragma unroll
+                for (int k = 0; k < 16 * LANES / 64; ++k) {
+                    const int row = k * (64 / LANES) + lane / LANES, at16 = lane % LANES;
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * ROW + at16 * 16);
+                    if (t + row < a.rows) *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.y) + (t + row) * a.y_ld + n0 + at16 * 8) = v;
+                }
+                __builtin_amdgcn_wave_barrier();
+            } else if (t + r < a.rows) {
+#pragma unroll
+                for (int j = 0; j < NB; ++j) quant_store4(a, t + r, n0 + 16 * j + 4 * g, y[j]);
+            }
+        }
+        if (!more) return;
     }
 }
 
 template <int WM, int WN, int MB, int NB, int NS, int WS>
-void launch_tiles(const QuantLinearArgs& a, hipStream_t st) {
+void launch_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
     constexpr int BM = 16 * WM * MB, BN = 16 * WN * NB;
     const int m_tiles = (a.rows + BM - 1) / BM, n_tiles = (a.cols + BN - 1) / BN;
-    hipLaunchKernelGGL((cats_quant_linear_tiles<WM, WN, MB, NB, NS, WS>), dim3(static_cast<unsigned>(m_tiles) * n_tiles),
+    hipLaunchKernelGGL((cats_quant_linear_tiles<WM, WN, MB, NB, NS, WS>), dim3(std::min(m_tiles * n_tiles, n_cus)),
                        dim3(64 * WM * WN), 0, st, a, m_tiles, n_tiles);
 }
 
 }  // namespace
 
-void launch_quant_tiles(const QuantLinearArgs& a, hipStream_t st) { launch_tiles<2, 4, 8, 4, 4, 4>(a, st); }
-void launch_quant_tiles_half(const QuantLinearArgs& a, hipStream_t st) { launch_tiles<2, 4, 4, 4, 4, 4>(a, st); }
+void launch_quant_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st) { launch_tiles<2, 4, 8, 4, 4, 4>(a, n_cus, st); }
+void launch_quant_tiles_half(const QuantLinearArgs& a, int n_cus, hipStream_t st) { launch_tiles<2, 4, 4, 4, 4, 4>(a, n_cus, st); }

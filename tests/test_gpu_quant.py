@@ -268,6 +268,13 @@ def test_linear_every_tile(tile, inner, dtype):
     run_linear(*TILE_SIZES[tile], inner, dtype)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols,inner", [(4001, 4177, 333), (3800, 8200, 1290), (300, 43501, 333), (513, 33000, 600)])
+def test_linear_several_tiles_a_workgroup(rows, cols, inner, dtype):
+    """More of the largest tiles than compute units: a workgroup's next tile is under way while it stores one."""
+    run_linear(rows, cols, inner, dtype)
+
+
 @pytest.mark.parametrize("rows", [1, 40, 130, 520])
 @pytest.mark.parametrize("x_ld,y_ld", [(1024, 1003), (1040, 1004), (1008, 1024)])
 def test_linear_strides(rows, x_ld, y_ld):

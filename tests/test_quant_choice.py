@@ -34,6 +34,13 @@ def test_every_tile_has_its_gpu_case(rule):
         assert rows % want[0] and cols % want[1]   # no size is a whole number of tiles
 
 
+def test_several_tiles_a_workgroup(rule):
+    """The sizes of the GPU test of that name: more of the two largest tiles than compute units."""
+    for rows, cols, want in ((4001, 4177, (256, 256)), (3800, 8200, (256, 256)), (300, 43501, (128, 256)), (513, 33000, (256, 256))):
+        assert tile(rule, rows, cols) == want
+        assert -(-rows // want[0]) * -(-cols // want[1]) > 256
+
+
 def test_kernels_stand_in_the_order_of_the_tiles(rule):
     """launch_quant_linear's list: <row blocks, column blocks, ...> of 16, then the two of the other kernel."""
     text = (host_shim.CSRC / "quant_linear.hip").read_text()
