@@ -14,9 +14,17 @@ namespace {
 // operands; register r of lane l of the result is D[row 4 (l / 16) + r of the first][row l % 16 of the second].  The
 // weights are the first operand: a lane's four results are neighbouring columns of y.
 
-// A workgroup owns a tile of 16 MB rows and 16 NB columns; its KW waves take turns at the steps of 128 values of k and add
-// up their sums through LDS at the end.  Each wave keeps NS of its steps in a ring of LDS that nobody else touches: it waits
-// for its own copies only, reads a step's fragments, sends for the step that takes their place, and multiplies.
+// From one row to some hundreds.  A workgroup owns a tile of 16 MB rows and 16 NB columns; its KW waves take turns at the steps
+// of 128 values of k and add up their sums through LDS at the end.  Each wave keeps NS of its steps in a ring of LDS that nobody
+// else touches: it waits for its own copies only, reads a step's fragments, sends for the step that takes their place, and
+// multiplies; there is no barrier before the sums meet.
+// Bound by the operands' way into the compute unit: with few rows the weights' from memory (22016 x 4096 weights: 14.7 us with
+// one row = 6.1 TB/s, 19.5 with 63 rows), with more the rows' and the weights' from the L2 (see quant_choice.hpp).
+// Splitting k over the waves, not over workgroups, needs no scratch memory and no second launch; X and W both go through LDS because
+// then every wait is for a count of copies that is known here (a load that the compiler sees in between makes it wait for
+// more), and eight lanes copy a whole line of a row of X.
+// A ring of one step and more workgroups a compute unit beat deeper rings for all tiles but 64 x 32 (256 x 4096 x 4096, 64 x 64:
+// 9.8 against 9.9 us, 512 rows 16.2 against 18.2).
 template <int MB, int NB, int KW, int NS>
 __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearArgs a, int m_tiles, int n_tiles) {
     constexpr int COPIES = 2 * (MB + NB), STEP = COPIES * 1024;   // of a step: copies of 1 KB, bytes
@@ -129,19 +137,26 @@ void launch_split(const QuantLinearArgs& a, int, hipStream_t st) {
                        st, a, m_tiles, n_tiles);
 }
 
-// One wave moves one kilobyte: rows of 64 values in, an operand of the matrix instruction out.
+// One wave moves one kilobyte: rows of 64 values in, an operand of the matrix instruction out.  vec: rows start at multiples of
+// 16 bytes.  (22016 x 4096: 108 us byte by byte, 28 us with whole loads.)
 __global__ __launch_bounds__(256) void cats_quant_pack(const int8_t* src, int64_t ld, int8_t* dst, int rows, int cols, int chunks,
-                                                      int64_t frags) {
+                                                      int64_t frags, bool vec) {
     const int lane = threadIdx.x & 63;
     for (int64_t f = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); f < frags; f += static_cast<int64_t>(gridDim.x) * 4) {
         const int rb = static_cast<int>(f / chunks), c = static_cast<int>(f - static_cast<int64_t>(rb) * chunks);
         const int n = rb * QPACK_ROWS + (lane & 15), k = c * QPACK_COLS + (lane >> 4) * 16;
         uint32_t v[4] = {0, 0, 0, 0};
         if (n < rows) {
-            const int8_t* p = src + n * ld;
+            const int8_t* p = src + n * ld + k;
+            if (vec && k + 16 <= cols) {
+                const u32x4 whole = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (k + e < cols) v[e >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(p[k + e])) << 8 * (e & 3);
+                for (int e = 0; e < 4; ++e) v[e] = whole[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (k + e < cols) v[e >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(p[e])) << 8 * (e & 3);
+            }
         }
         *reinterpret_cast<u32x4*>(dst + f * QPACK_FRAG + lane * 16) = u32x4{v[0], v[1], v[2], v[3]};
     }
@@ -189,7 +204,7 @@ int cats_pack_quantized_matrix(const int8_t* src, int64_t src_ld, int32_t rows, 
     if (cols > CATS_QUANT_MAX_INNER || rows > CATS_QUANT_MAX_ROWS) return CATS_ECAPACITY;
     const int64_t frags = frags_of(rows, cols);
     hipLaunchKernelGGL(cats_quant_pack, dim3(static_cast<unsigned>(std::min<int64_t>((frags + 3) / 4, 1 << 16))), dim3(256), 0, static_cast<hipStream_t>(stream),
-                       src, src_ld, dst, rows, cols, qpack_chunks(cols), frags);
+                       src, src_ld, dst, rows, cols, qpack_chunks(cols), frags, aligned16(src) && src_ld % 16 == 0);
     return hipGetLastError() == hipSuccess ? CATS_OK : CATS_EHIP;
 }
 

@@ -311,8 +311,8 @@ def test_linear_scales_next_to_the_range():
 
 def test_pack_layout():
     rng = rng_of(7)
-    for rows, cols in [(16, 64), (5, 3), (33, 130), (100, 1001)]:
-        w = whole_numbers(rng, rows, cols)
+    for rows, cols, ld in [(16, 64, 64), (5, 3, 16), (33, 130, 144), (100, 1001, 1008), (100, 1001, 1003), (20, 64, 65), (17, 320, 320)]:
+        w = whole_numbers(rng, rows, cols, ld=ld)
         packed = cats.cats_pack_quantized_matrix(w).cpu().numpy()
         full = np.zeros(((rows + 15) // 16 * 16, (cols + 255) // 256 * 256), np.int8)
         full[:rows, :cols] = w.cpu().numpy()
