@@ -28,7 +28,7 @@ namespace {
 template <int MB, int NB, int KW, int NS>
 __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearArgs a, int m_tiles, int n_tiles) {
     constexpr int COPIES = 2 * (MB + NB), STEP = COPIES * 1024;   // of a step: copies of 1 KB, bytes
-    static_assert((NS - 1) * COPIES < 64, "vmcnt");
+    static_assert(NS <= 2 && (NS - 1) * COPIES < 64, "counts of the waits");
     constexpr int RING = KW * NS * STEP;
     // the waves' sums meet in parts of PB row blocks that fit where the ring was
     constexpr int PB = KW * MB * NB * 1024 <= RING ? MB : MB / 2;
@@ -79,13 +79,9 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
         if (i < mine) fetch(i, i);
     int slot = 0;
     for (int i = 0; i < mine; ++i) {
-        const int behind = mine - 1 - i;   // steps that are under way behind this one, at most NS - 1
-        if (behind >= NS - 1)
+        // this step's copies; of the NS - 1 behind it all are under way until the last ones
+        if (mine - 1 - i >= NS - 1)
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 1) * COPIES) : "memory");
-        else if (NS > 2 && behind == 2)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NS > 3 ? 2 * COPIES : 0) : "memory");
-        else if (behind == 1)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NS > 2 ? COPIES : 0) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         const int8_t* from = &s_lds[0] + (wave * NS + slot) * STEP;
@@ -203,8 +199,9 @@ int cats_pack_quantized_matrix(const int8_t* src, int64_t src_ld, int32_t rows, 
     if (!src || !dst || !aligned16(dst) || rows < 1 || cols < 1 || src_ld < cols) return CATS_EINVAL;
     if (cols > CATS_QUANT_MAX_INNER || rows > CATS_QUANT_MAX_ROWS) return CATS_ECAPACITY;
     const int64_t frags = frags_of(rows, cols);
-    hipLaunchKernelGGL(cats_quant_pack, dim3(static_cast<unsigned>(std::min<int64_t>((frags + 3) / 4, 1 << 16))), dim3(256), 0, static_cast<hipStream_t>(stream),
-                       src, src_ld, dst, rows, cols, qpack_chunks(cols), frags, aligned16(src) && src_ld % 16 == 0);
+    const unsigned groups = static_cast<unsigned>(std::min<int64_t>((frags + 3) / 4, 1 << 16));
+    hipLaunchKernelGGL(cats_quant_pack, dim3(groups), dim3(256), 0, static_cast<hipStream_t>(stream), src, src_ld, dst, rows, cols,
+                       qpack_chunks(cols), frags, aligned16(src) && src_ld % 16 == 0);
     return hipGetLastError() == hipSuccess ? CATS_OK : CATS_EHIP;
 }
 

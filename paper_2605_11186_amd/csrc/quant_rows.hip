@@ -7,9 +7,13 @@
 // than 20 instructions a value: the kernel is bound by memory with many rows and by its chain of loads, two reductions and
 // stores with few.  8192 x 5120 with a bf16 delta 85 us, 32000 x 4096 from bf16 68 us, SwiGLU of 4096 x 13824 53 us: 5.4 to 5.8
 // TB/s, where a large copy reaches 5.2; 63 rows of 4096 2.3 to 2.9 us, where an empty launch takes 1.6.
+#include <type_traits>
+
 #include "quant.hpp"
 
 namespace {
+
+typedef double none_t;   // the type of a delta that is not there
 
 constexpr float SCALE_MIN = 0x1p-126f;   // smallest normal number: 1 / scale stays finite
 
@@ -81,12 +85,12 @@ __device__ __forceinline__ Raw<T, VEC> load8(const T* row, int tid, int j, int c
 }
 
 // TPR threads share a row (64: four rows a workgroup), NC pieces of 8 values each.  T: type of the source.
-// D: type of delta (void: none).
+// D: type of delta (none_t: none).
 template <int KIND, class T, class D, int TPR, int NC, bool VEC>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kernel(QuantRowsArgs a) {
     constexpr int ROWS_WG = TPR < 256 ? 256 / TPR : 1;
     constexpr int WAVES = TPR / 64;
-    constexpr bool HAS_DELTA = sizeof(D) < 8;
+    constexpr bool HAS_DELTA = !std::is_same<D, none_t>::value;
     const int tid = threadIdx.x % TPR;
     const int t = blockIdx.x * ROWS_WG + threadIdx.x / TPR;
     if (t >= a.rows) return;   // whole waves, and no barrier where a workgroup has several rows
@@ -261,15 +265,13 @@ template <int KIND, class T, class D>
 void by_alignment(const QuantRowsArgs& a, hipStream_t st) {
     bool vec = a.cols % 8 == 0 && whole_pieces(a.src, a.src_ld, sizeof(T)) && whole_pieces(a.q, a.q_ld, 1);
     if (KIND == ROWS_NORM) vec = vec && whole_pieces(a.gain, 0, 2);
-    if (KIND == ROWS_NORM && sizeof(D) < 8)
+    if (KIND == ROWS_NORM && !std::is_same<D, none_t>::value)
         vec = vec && whole_pieces(a.delta, a.delta_ld, sizeof(D)) && whole_pieces(a.x_out, a.x_out_ld, 4);
     if (vec)
         by_size<KIND, T, D, true>(a, st);
     else
         by_size<KIND, T, D, false>(a, st);
 }
-
-typedef double none_t;   // no delta
 
 bool type_ok(int32_t t) { return t == CATS_F32 || t == CATS_BF16; }
 bool aligned(const void* p, int32_t type) { return reinterpret_cast<uintptr_t>(p) % (type == CATS_F32 ? 4 : 2) == 0; }

@@ -97,10 +97,10 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
     // u: parity of the step
     auto step = [&](int s, int slot, auto u_) {
         constexpr int u = decltype(u_)::value;
-        // Requests are dealt out over the step, one between some products each: issued together they hold up the products behind
-        // them (49 -> 43 us for 256 x 4096 x 4096).  Copies of step s - 2 and before, that is for step s + 1, are older than
-        // all that step s - 1 issued; then everybody's are there, and nobody reads the slot of step s - 1 any
-        // more: the copies for step s + NS - 1 go there (those of
+        // Requests are dealt out over the step, one between some products each: issued together they hold up the products
+        // behind them (49 -> 43 us for 256 x 4096 x 4096).
+        // What step s - 1 issued may be under way; all before it, the copies for step s + 1 among it, has come.  Then everybody's
+        // copies are there, and nobody reads the slot of step s - 1 any more: the copies for step s + NS - 1 go there (those of
         // steps that do not exist are read by nobody).
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)" ::"n"(COPIES + 2 * NB), "n"(AHEAD) : "memory");
         __builtin_amdgcn_s_barrier();

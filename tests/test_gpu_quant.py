@@ -354,6 +354,25 @@ def test_offsets_beyond_32_bits():
         check_linear(x, sx, w[:70], sw[:70], y[:, :70])
 
 
+def test_most_rows_and_most_columns():
+    most = cats.CATS_QUANT_MAX_ROWS
+    src = torch.randn(most, 8, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    q, _ = padded(most, 8, torch.int8)
+    scale = torch.empty(most, device="cuda")
+    cats.cats_quantize_rows(src, q, scale)
+    check_rows(f64(src), q, scale, 0.0)
+    w = whole_numbers(rng_of(13), 3, 8)
+    y, sw = torch.empty(most, 3, device="cuda"), torch.full((3,), 1e-3, device="cuda")
+    cats.cats_quantized_linear(q, scale, cats.cats_pack_quantized_matrix(w), sw, y)
+    check_linear(q, scale, w, sw, y)
+    del src, y
+    x = whole_numbers(rng_of(14), 2, 16)   # and the other way round
+    y, one = torch.empty(2, most, device="cuda"), torch.ones(2, device="cuda")
+    w = torch.randint(-128, 128, (most, 16), dtype=torch.int8, device="cuda")
+    cats.cats_quantized_linear(x, one, cats.cats_pack_quantized_matrix(w), scale, y)
+    check_linear(x, one, w, scale, y)
+
+
 # ---------------------------------------------------------------- use
 def test_no_rows():
     q, s = torch.empty(0, 64, dtype=torch.int8, device="cuda"), torch.empty(0, device="cuda")

@@ -69,6 +69,11 @@ def test_quantized_linear(changed, status):
     assert call("cats_quantized_linear", LINEAR, **changed) == status
 
 
+def test_layers_need_a_context():
+    layers = (cats.QuantizedLayer * 1)()
+    assert cats.library().cats_verify_layers_quantized(None, layers, 0, 1, P, P, 0, None) == E
+
+
 def test_packed_bytes():
     assert cats.cats_packed_quantized_bytes(1, 1) == 4096
     assert cats.cats_packed_quantized_bytes(16, 256) == 4096
