@@ -12,7 +12,7 @@ struct QuantTile {
 };
 constexpr QuantTile QUANT_TILES[] = {{16, 16, 32},   {16, 32, 48},   {32, 32, 64},    {64, 32, 96},   {64, 48, 112},
                                      {64, 64, 128},  {64, 96, 160},  {64, 112, 176},  {96, 96, 192},  {128, 64, 192},
-                                     {128, 96, 250}, {128, 128, 350}, {128, 256, 500}, {256, 256, 700}};
+                                     {128, 96, 250}, {96, 128, 288}, {128, 128, 350}, {128, 256, 500}, {256, 256, 700}};
 constexpr int N_QUANT_TILES = sizeof(QUANT_TILES) / sizeof(QUANT_TILES[0]);
 inline int quant_tile_choice(int rows, int cols, int n_cus) {
     int best = 0;

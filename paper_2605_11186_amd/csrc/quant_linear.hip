@@ -184,7 +184,7 @@ void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
     static constexpr void (*LAUNCH[])(const QuantLinearArgs&, int, hipStream_t) = {
         launch_split<1, 1, 8, 1>, launch_split<1, 2, 8, 1>, launch_split<2, 2, 8, 1>, launch_split<4, 2, 4, 2>, launch_split<4, 3, 4, 1>,
         launch_split<4, 4, 4, 1>, launch_split<4, 6, 4, 1>, launch_split<4, 7, 4, 1>, launch_split<6, 6, 4, 1>, launch_split<8, 4, 4, 1>,
-        launch_split<8, 6, 4, 1>, launch_split<8, 8, 4, 1>, launch_quant_tiles_half,  launch_quant_tiles};
+        launch_split<8, 6, 4, 1>, launch_split<6, 8, 4, 1>, launch_split<8, 8, 4, 1>, launch_quant_tiles_half,  launch_quant_tiles};
     static_assert(sizeof(LAUNCH) / sizeof(LAUNCH[0]) == N_QUANT_TILES, "one kernel for each tile");
     LAUNCH[quant_tile_choice(a.rows, a.cols, n_cus)](a, n_cus, st);
 }

@@ -258,7 +258,7 @@ def test_linear(rows, cols, inner, dtype):
 # one size for each tile that a product is cut into on 256 compute units (tests/test_quant_choice.py), none of them whole
 TILE_SIZES = {(16, 16): (13, 1003), (16, 32): (9, 4107), (32, 32): (30, 4107), (64, 32): (62, 4107), (64, 48): (57, 10007),
               (64, 64): (254, 4077), (64, 96): (61, 21001), (64, 112): (61, 27001), (96, 96): (95, 21001), (128, 64): (509, 4077),
-              (128, 96): (125, 21001), (128, 128): (1021, 4077), (128, 256): (2001, 4077), (256, 256): (4001, 4077)}
+              (128, 96): (125, 21001), (96, 128): (763, 4077), (128, 128): (1021, 4077), (128, 256): (2001, 4077), (256, 256): (4001, 4077)}
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
