@@ -401,15 +401,17 @@ def _refuse_operands(device, **operands):
 
 
 def _stream_on(device, stream):
-    """A stream's handle; a torch stream has to belong to the tensors' device."""
-    if stream is not None and getattr(stream, "device_index", device) != device:
+    """A stream's handle (a torch stream's or the number itself); a torch stream has to belong to the tensors' device."""
+    if stream is None:
+        return None
+    if getattr(stream, "device_index", device) != device:
         raise CatsError(CATS_EINVAL, f"stream of device {stream.device_index}, tensors on device {device}")
-    return _stream(stream)
+    return getattr(stream, "cuda_stream", stream)
 
 
-def _row_stride(stride, rows, cols):
-    # the stride of a single row says nothing: any that suits a row of this length will do
-    return stride if rows > 1 else (cols + 15) // 16 * 16
+# The stride of a single row says nothing: any that suits a row of this length will do.
+def _single_row(cols):
+    return (cols + 15) // 16 * 16
 
 
 def cats_quantize_rows(src, q_out, scale_out, stream=None):
@@ -425,8 +427,10 @@ def cats_quantize_rows(src, q_out, scale_out, stream=None):
         _refuse_operands(dev, src=(src, (_f32, _bf16), (rows, cols)), q_out=(q_out, _i8, (rows, cols)),
                          scale_out=(scale_out, _f32, (rows,)))
     if rows:
-        _check(library().cats_quantize_rows(src.data_ptr(), code, _row_stride(ld, rows, cols), rows, cols, q_out.data_ptr(),
-                                                 _row_stride(q_ld, rows, cols), scale_out.data_ptr(), _stream_on(dev, stream)))
+        if rows == 1:
+            ld = q_ld = _single_row(cols)
+        _check(library().cats_quantize_rows(src.data_ptr(), code, ld, rows, cols, q_out.data_ptr(), q_ld, scale_out.data_ptr(),
+                                            _stream_on(dev, stream)))
 
 
 def cats_rmsnorm_quantize(x, gain, eps: float, q_out, scale_out, delta=None, x_out=None, stream=None):
@@ -442,7 +446,6 @@ def cats_rmsnorm_quantize(x, gain, eps: float, q_out, scale_out, delta=None, x_o
         out = x if x_out is None else x_out
         (d_ld, d_step), (o_ld, o_step) = delta.stride(), out.stride()
         d_code, d_ptr, o_ptr = _code_of.get(delta.dtype), delta.data_ptr(), out.data_ptr()
-        d_ld, o_ld = _row_stride(d_ld, rows, cols), _row_stride(o_ld, rows, cols)
         ok = (d_code is not None and delta.shape == shape and out.shape == shape and out.dtype is _f32 and
               (cols == 1 or d_step == o_step == 1) and delta.get_device() == dev and out.get_device() == dev)
     elif x_out is not None:
@@ -456,9 +459,10 @@ def cats_rmsnorm_quantize(x, gain, eps: float, q_out, scale_out, delta=None, x_o
         _refuse_operands(dev, x=(x, _f32, (rows, cols)), gain=(gain, _bf16, (cols,)), q_out=(q_out, _i8, (rows, cols)),
                          scale_out=(scale_out, _f32, (rows,)), **more)
     if rows:
-        _check(library().cats_rmsnorm_quantize(x.data_ptr(), _row_stride(ld, rows, cols), d_ptr, d_code, d_ld, gain.data_ptr(),
-                                                    eps, rows, cols, o_ptr, o_ld, q_out.data_ptr(), _row_stride(q_ld, rows, cols),
-                                                    scale_out.data_ptr(), _stream_on(dev, stream)))
+        if rows == 1:
+            ld = q_ld = d_ld = o_ld = _single_row(cols)
+        _check(library().cats_rmsnorm_quantize(x.data_ptr(), ld, d_ptr, d_code, d_ld, gain.data_ptr(), eps, rows, cols, o_ptr, o_ld,
+                                               q_out.data_ptr(), q_ld, scale_out.data_ptr(), _stream_on(dev, stream)))
 
 
 def cats_swiglu_quantize(gate_up, q_out, scale_out, stream=None):
@@ -474,9 +478,10 @@ def cats_swiglu_quantize(gate_up, q_out, scale_out, stream=None):
         _refuse_operands(dev, gate_up=(gate_up, (_f32, _bf16), (rows, 2 * cols)), q_out=(q_out, _i8, (rows, cols)),
                          scale_out=(scale_out, _f32, (rows,)))
     if rows:
-        _check(library().cats_swiglu_quantize(gate_up.data_ptr(), code, _row_stride(ld, rows, 2 * cols), rows, cols,
-                                                   q_out.data_ptr(), _row_stride(q_ld, rows, cols), scale_out.data_ptr(),
-                                                   _stream_on(dev, stream)))
+        if rows == 1:
+            ld, q_ld = _single_row(2 * cols), _single_row(cols)
+        _check(library().cats_swiglu_quantize(gate_up.data_ptr(), code, ld, rows, cols, q_out.data_ptr(), q_ld, scale_out.data_ptr(),
+                                              _stream_on(dev, stream)))
 
 
 def cats_packed_quantized_bytes(rows: int, cols: int) -> int:
@@ -493,8 +498,9 @@ def cats_pack_quantized_matrix(src, stream=None):
     if src.dtype is not _i8 or (cols > 1 and step != 1) or dev < 0 or dev != _current_device():
         _refuse_operands(dev, src=(src, _i8, (rows, cols)))
     dst = torch.empty(cats_packed_quantized_bytes(rows, cols), dtype=torch.int8, device=src.device)
-    _check(library().cats_pack_quantized_matrix(src.data_ptr(), _row_stride(ld, rows, cols), rows, cols, dst.data_ptr(),
-                                                _stream_on(dev, stream)))
+    if rows == 1:
+        ld = _single_row(cols)
+    _check(library().cats_pack_quantized_matrix(src.data_ptr(), ld, rows, cols, dst.data_ptr(), _stream_on(dev, stream)))
     return dst
 
 
@@ -513,13 +519,13 @@ def cats_quantized_linear(x, x_scale, w_packed, w_scale, out, stream=None):
             w_packed.get_device() != dev or dev < 0 or dev != _current_device()):
         _refuse_operands(dev, x=(x, _i8, (rows, inner)), x_scale=(x_scale, _f32, (rows,)), w_packed=(w_packed, _i8, (packed,)),
                          w_scale=(w_scale, _f32, (cols,)), out=(out, (_f32, _bf16), (rows, cols)))
-    ld = _row_stride(ld, rows, inner)
+    if rows == 1:
+        ld, y_ld = _single_row(inner), _single_row(cols)
     if inner % 16 and x.untyped_storage().nbytes() < x.storage_offset() + (rows - 1) * ld + (inner + 15) // 16 * 16:
         raise CatsError(CATS_EINVAL, "x: its last row must be readable up to a multiple of 16 bytes")
     if rows:
         _check(library().cats_quantized_linear(x.data_ptr(), ld, x_scale.data_ptr(), w_packed.data_ptr(), w_scale.data_ptr(),
-                                                    out.data_ptr(), code, _row_stride(y_ld, rows, cols), rows, cols, inner,
-                                                    _stream_on(dev, stream)))
+                                               out.data_ptr(), code, y_ld, rows, cols, inner, _stream_on(dev, stream)))
 
 
 def quantize_layer(tensors: dict) -> dict:

@@ -4,8 +4,8 @@
 
 // A launch takes about as long as the compute unit with the most tiles needs for their operands, rows of X and of W alike:
 // rounds of tiles times (BM + BN).  Measured at inner = 4096 and 4096 columns (us): 1.2 + 0.065 rounds (BM + BN), within
-// 10 % from 63 to 512 rows, for the tiles of up to 128 x 64; the larger ones, which the matrix instructions bind, count as
-// what they measure in this unit.  (With few rows and many columns the weights' way from memory comes on top for all alike:
+// 10 % from 63 to 512 rows, for the tiles whose cost is BM + BN; the larger ones, which the matrix instructions bind, cost what
+// they measure in this unit.  (With few rows and many columns the weights' way from memory comes on top for all alike:
 // 90 MB of weights take 15 us with one row, 20 with 63.)
 struct QuantTile {
     int bm, bn, cost;   // rows, columns, cost of a round of one tile per compute unit
