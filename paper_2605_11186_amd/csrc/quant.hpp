@@ -46,8 +46,13 @@ void launch_quant_tiles_half(const QuantLinearArgs& a, int n_cus, hipStream_t st
 
 // 64 lanes copy 16 bytes each from base + their own offset to 1024 consecutive bytes of LDS (at byte `lds`), with no
 // register between.  Counted in vmcnt like a load; the compiler does not see it and waits for nothing on its account.
+// ONCE: of bytes that are not wanted again soon, which the caches need not keep.
+template <bool ONCE = false>
 __device__ __forceinline__ void copy_to_lds(const int8_t* base, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
 
 // Tile number `index` (of a launch's workgroups).  Workgroup b runs on XCD b % 8: an XCD takes a run of tiles, in bands of 4 row

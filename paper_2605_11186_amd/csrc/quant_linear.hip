@@ -25,7 +25,8 @@ namespace {
 // more), and eight lanes copy a whole line of a row of X.
 // A ring of one step and more workgroups a compute unit beat deeper rings for all tiles but 64 x 32 (256 x 4096 x 4096, 64 x 64:
 // 9.8 against 9.9 us, 512 rows 16.2 against 18.2).
-template <int MB, int NB, int KW, int NS>
+// ONCE: the weights are copied past the caches (see launch_split).
+template <int MB, int NB, int KW, int NS, bool ONCE>
 __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearArgs a, int m_tiles, int n_tiles) {
     constexpr int COPIES = 2 * (MB + NB), STEP = COPIES * 1024;   // of a step: copies of 1 KB, bytes
     static_assert(NS <= 2 && (NS - 1) * COPIES < 64, "counts of the waits");
@@ -62,8 +63,8 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
         const uint32_t to = lds0 + slot * STEP;
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            copy_to_lds(wp[j] + s * 2048, lane * 16, to + j * 2048);
-            copy_to_lds(wp[j] + s * 2048 + 1024, lane * 16, to + j * 2048 + 1024);
+            copy_to_lds<ONCE>(wp[j] + s * 2048, lane * 16, to + j * 2048);
+            copy_to_lds<ONCE>(wp[j] + s * 2048 + 1024, lane * 16, to + j * 2048 + 1024);
         }
 #pragma unroll
         for (int p = 0; p < 2 * MB; ++p) copy_to_lds(x0, xo[p] + k, to + NB * 2048 + p * 1024);
@@ -126,11 +127,17 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
     }
 }
 
+// Weights that one row tile reads, a third of the 256 MB cache in front of the memory or more of them, are copied past the
+// caches: they will hardly be found there by the next call, and the next matrix is.  63 x 27648 x 5120 33 -> 28.5 us; 63 x 22016 x
+// 4096 with twelve matrices in turn 22.8 -> 20.1, one row 17.2 -> 15.7, with three (270 MB) 19.9 -> 19.6.  Smaller ones may be of a
+// model that the cache holds: three of 4096 x 11008 in turn take 8.4 us with one row, past the caches 9.8.
+constexpr int64_t ONCE_BYTES = (int64_t{256} << 20) / 3;
 template <int MB, int NB, int KW, int NS>
 void launch_split(const QuantLinearArgs& a, int, hipStream_t st) {
     const int m_tiles = (a.rows + 16 * MB - 1) / (16 * MB), n_tiles = (a.cols + 16 * NB - 1) / (16 * NB);
-    hipLaunchKernelGGL((cats_quant_linear_split<MB, NB, KW, NS>), dim3(static_cast<unsigned>(m_tiles) * n_tiles), dim3(64 * KW), 0,
-                       st, a, m_tiles, n_tiles);
+    const bool once = m_tiles == 1 && static_cast<int64_t>(a.cols) * a.inner >= ONCE_BYTES;
+    hipLaunchKernelGGL((once ? cats_quant_linear_split<MB, NB, KW, NS, true> : cats_quant_linear_split<MB, NB, KW, NS, false>),
+                       dim3(static_cast<unsigned>(m_tiles) * n_tiles), dim3(64 * KW), 0, st, a, m_tiles, n_tiles);
 }
 
 // One wave moves one kilobyte: rows of 64 values in, an operand of the matrix instruction out.  vec: rows start at multiples of

@@ -268,6 +268,18 @@ def test_linear_every_tile(tile, inner, dtype):
     run_linear(*TILE_SIZES[tile], inner, dtype)
 
 
+# few rows and some hundred megabytes of weights, which pass the caches by: one size for each tile that takes them all in one row tile
+ONCE_SIZES = {(16, 16): (9, 4077, 22001), (16, 32): (3, 22001, 4099), (32, 32): (29, 4107, 22001), (64, 32): (59, 4107, 22001),
+              (64, 48): (57, 10007, 9003), (64, 64): (61, 15307, 6003), (64, 96): (61, 21001, 4301), (64, 112): (61, 27001, 3401),
+              (96, 96): (95, 21001, 4301), (128, 64): (125, 15307, 6003), (128, 96): (125, 21001, 4301), (96, 128): (95, 32001, 2807),
+              (128, 128): (125, 27001, 3401)}
+
+
+@pytest.mark.parametrize("tile", sorted(ONCE_SIZES))
+def test_linear_weights_past_the_caches(tile):
+    run_linear(*ONCE_SIZES[tile], torch.bfloat16)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("rows,cols,inner", [(4001, 4177, 333), (3800, 8200, 1290), (300, 43501, 333), (513, 33000, 600)])
 def test_linear_several_tiles_a_workgroup(rows, cols, inner, dtype):

@@ -5,7 +5,7 @@ import re
 import pytest
 
 import host_shim
-from test_gpu_quant import TILE_SIZES
+from test_gpu_quant import ONCE_SIZES, TILE_SIZES
 
 SHIM = """
 #include "quant_choice.hpp"
@@ -32,6 +32,14 @@ def test_every_tile_has_its_gpu_case(rule):
     for want, (rows, cols) in TILE_SIZES.items():
         assert tile(rule, rows, cols) == want
         assert rows % want[0] and cols % want[1]   # no size is a whole number of tiles
+
+
+def test_sizes_whose_weights_pass_the_caches(rule):
+    """The sizes of that GPU test: one row tile, more than a third of 256 MB of weights."""
+    for want, (rows, cols, inner) in ONCE_SIZES.items():
+        assert tile(rule, rows, cols) == want, (rows, cols, tile(rule, rows, cols))
+        assert rows <= want[0] and cols * inner >= (256 << 20) // 3
+    assert sorted(ONCE_SIZES) == sorted(t for t in TILE_SIZES if t[0] <= 128 and t != (128, 256))
 
 
 def test_several_tiles_a_workgroup(rule):
