@@ -509,7 +509,8 @@ void enqueue_norm_quantized(cats_ctx* c, float* x, bool delta, const void* gain,
     a.x_out_ld = H;
     launch_quant_rows(a, ROWS_NORM, st);
 }
-void enqueue_linear_quantized(cats_ctx* c, const void* q, int inner, const int8_t* w, const float* w_scale, int cols, hipStream_t st) {
+void enqueue_linear_quantized(cats_ctx* c, const void* q, int inner, const int8_t* w, const float* w_scale, int cols, bool cold,
+                              hipStream_t st) {
     QuantLinearArgs a{};
     a.x = static_cast<const int8_t*>(q);
     a.x_ld = inner;
@@ -523,14 +524,16 @@ void enqueue_linear_quantized(cats_ctx* c, const void* q, int inner, const int8_
     a.cols = cols;
     a.inner = inner;
     a.chunks = qpack_chunks(inner);
+    a.cold = cold;
     launch_quant_linear(a, c->n_cus, st);
 }
-// One layer; delta: the layer before has left its last product in c->part, still to be added to x, as this one does.
-void enqueue_layer_quantized(cats_ctx* c, const cats_quantized_layer* w, float* x, bool delta, const cats_kv_layer* kv, int ctx_len,
-                             hipStream_t st) {
+// One layer; delta: the layer before has left its last product in c->part, still to be added to x, as this one does.  cold: see
+// QuantLinearArgs.
+void enqueue_layer_quantized(cats_ctx* c, const cats_quantized_layer* w, float* x, bool delta, bool cold, const cats_kv_layer* kv,
+                             int ctx_len, hipStream_t st) {
     const int H = c->d.hidden, F = c->d.ffn;
     enqueue_norm_quantized(c, x, delta, w->g_attn, st);
-    enqueue_linear_quantized(c, c->xn, H, w->w_qkv, w->s_qkv, 3 * H, st);
+    enqueue_linear_quantized(c, c->xn, H, w->w_qkv, w->s_qkv, 3 * H, cold, st);
     QkvRopeArgs qa;
     qa.part = c->part;
     qa.plan = GemmPlan{1, GEMM_KC, 1, 1, 1};   // one complete piece
@@ -555,11 +558,11 @@ void enqueue_layer_quantized(cats_ctx* c, const cats_quantized_layer* w, float* 
     QuantRowsArgs a = quant_rows(c, c->attn, H, H, c->xn);
     a.src_type = CATS_BF16;
     launch_quant_rows(a, ROWS_PLAIN, st);
-    enqueue_linear_quantized(c, c->xn, H, w->w_o, w->s_o, H, st);
+    enqueue_linear_quantized(c, c->xn, H, w->w_o, w->s_o, H, cold, st);
     enqueue_norm_quantized(c, x, true, w->g_ffn, st);
-    enqueue_linear_quantized(c, c->xn, H, w->w_gate_up, w->s_gate_up, 2 * F, st);
+    enqueue_linear_quantized(c, c->xn, H, w->w_gate_up, w->s_gate_up, 2 * F, cold, st);
     launch_quant_rows(quant_rows(c, c->part, 2 * static_cast<int64_t>(F), F, c->hact), ROWS_SWIGLU, st);
-    enqueue_linear_quantized(c, c->hact, F, w->w_down, w->s_down, H, st);
+    enqueue_linear_quantized(c, c->hact, F, w->w_down, w->s_down, H, cold, st);
 }
 
 RopeTableArgs rope_table_args(const cats_ctx* c, int ctx_len) {
@@ -908,8 +911,11 @@ int cats_verify_layers_quantized(cats_ctx* ctx, const cats_quantized_layer* laye
     }
     hipStream_t st = as_stream(stream);
     launch_rope_table(rope_table_args(ctx, ctx_len), st);
+    // weights that the call reads: 4 H^2 + 3 H F bytes a layer, against a cache of 256 MB
+    const int64_t H = ctx->d.hidden, F = ctx->d.ffn;
+    const bool cold = (4 * H * H + 3 * H * F) * (layer_end - layer_begin) > int64_t{256} << 20;
     for (int l = layer_begin; l < layer_end; ++l)
-        enqueue_layer_quantized(ctx, &layers[l], hidden, l > layer_begin, &kv[l], ctx_len, st);
+        enqueue_layer_quantized(ctx, &layers[l], hidden, l > layer_begin, cold, &kv[l], ctx_len, st);
     ResidualNormArgs rn;   // the last layer's product
     rn.x = hidden;
     rn.x_in = nullptr;

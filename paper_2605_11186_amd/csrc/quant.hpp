@@ -39,6 +39,7 @@ struct QuantLinearArgs {
     int rows, cols, inner;
     int chunks;            // packed chunks of 64 along inner, a multiple of four
     int y_type;
+    bool cold = false;     // the caller reads more weights than the caches hold before it reads these again
 };
 void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st);
 void launch_quant_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st);        // tiles of 256 x 256
@@ -46,7 +47,7 @@ void launch_quant_tiles_half(const QuantLinearArgs& a, int n_cus, hipStream_t st
 
 // 64 lanes copy 16 bytes each from base + their own offset to 1024 consecutive bytes of LDS (at byte `lds`), with no
 // register between.  Counted in vmcnt like a load; the compiler does not see it and waits for nothing on its account.
-// ONCE: of bytes that are not wanted again soon, which the caches need not keep.
+// ONCE: of bytes that are not wanted again soon and that the caches need not keep.
 template <bool ONCE = false>
 __device__ __forceinline__ void copy_to_lds(const int8_t* base, uint32_t offset, uint32_t lds) {
     if constexpr (ONCE)

@@ -127,15 +127,16 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
     }
 }
 
-// Weights that one row tile reads, a third of the 256 MB cache in front of the memory or more of them, are copied past the
-// caches: they will hardly be found there by the next call, and the next matrix is.  63 x 27648 x 5120 33 -> 28.5 us; 63 x 22016 x
-// 4096 with twelve matrices in turn 22.8 -> 20.1, one row 17.2 -> 15.7, with three (270 MB) 19.9 -> 19.6.  Smaller ones may be of a
-// model that the cache holds: three of 4096 x 11008 in turn take 8.4 us with one row, past the caches 9.8.
-constexpr int64_t ONCE_BYTES = (int64_t{256} << 20) / 3;
+// Weights that will hardly be found in the 256 MB cache in front of the memory by the next call are copied past the caches, which then
+// keep other things: a matrix of a third of that size or more that one row tile reads, and whatever the caller calls cold, also
+// for two tiles of up to 32 rows (which read it side by side; larger pairs lose by it).  64 x 27648 x 5120 33 -> 28.5 us; 63 x 22016 x 4096 with twelve matrices in turn
+// 22.8 -> 20.1, one row 17.2 -> 15.7, with three (270 MB) 19.9 -> 19.6; 63 x 4096 x 11008, forty in turn, 17.3 -> 15.5.  Smaller
+// ones may be of a model that the cache holds: three of 4096 x 11008 in turn take 8.4 us with one row, past the caches 9.8.
+constexpr int64_t CACHE_BYTES = int64_t{256} << 20;
 template <int MB, int NB, int KW, int NS>
 void launch_split(const QuantLinearArgs& a, int, hipStream_t st) {
     const int m_tiles = (a.rows + 16 * MB - 1) / (16 * MB), n_tiles = (a.cols + 16 * NB - 1) / (16 * NB);
-    const bool once = m_tiles == 1 && static_cast<int64_t>(a.cols) * a.inner >= ONCE_BYTES;
+    const bool once = a.cold ? m_tiles <= (MB <= 2 ? 2 : 1) : m_tiles == 1 && static_cast<int64_t>(a.cols) * a.inner >= CACHE_BYTES / 3;
     hipLaunchKernelGGL((once ? cats_quant_linear_split<MB, NB, KW, NS, true> : cats_quant_linear_split<MB, NB, KW, NS, false>),
                        dim3(static_cast<unsigned>(m_tiles) * n_tiles), dim3(64 * KW), 0, st, a, m_tiles, n_tiles);
 }

@@ -142,6 +142,38 @@ def test_layers(model, nodes, ctx_len):
     assert torch.equal(again, hidden)
 
 
+@pytest.mark.parametrize("nodes", [1, 20, 63, 128])
+def test_a_call_whose_weights_pass_the_caches(nodes):
+    """Two layers of 202 MB of weights in one call (past the caches) and one after the other (through them): the same bits."""
+    d = synth.V7B
+    gen = torch.Generator(device="cuda").manual_seed(17)
+
+    def matrix(rows, cols):
+        return torch.empty(rows, cols, device="cuda").normal_(0, 0.02, generator=gen).to(torch.bfloat16)
+
+    H, F, one = d.hidden, d.ffn, torch.ones(d.hidden, dtype=torch.bfloat16, device="cuda")
+    layers = [cats.quantize_layer(dict(wq=matrix(H, H), wk=matrix(H, H), wv=matrix(H, H), wo=matrix(H, H), w_gate=matrix(F, H),
+                                       w_up=matrix(F, H), w_down=matrix(H, F), g_attn=one, g_ffn=one)) for _ in range(2)]
+    ctx = cats.cats_create(cats.ModelDesc(2, H, d.n_heads, d.head_dim, F, d.vocab, 256, 128, d.rms_eps, d.rope_base, 0))
+    try:
+        parent, depth = tree_of(nodes, 4)
+        cats.cats_set_tree(ctx, np.zeros(nodes, np.int32), parent, depth)
+        ks = [torch.zeros(d.n_heads, 256, d.head_dim, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        vs = [torch.zeros(d.n_heads, d.head_dim, 256, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        arr, kv = cats.quantized_layer_array(layers), cats.kv_array(ks, vs)
+        x = torch.empty(nodes, H, device="cuda").normal_(generator=gen)
+        both, each = x.clone(), x.clone()
+        cats.cats_verify_layers_quantized(ctx, arr, 0, 2, both, kv, 40)
+        rows = [t.clone() for t in ks + vs]
+        for l in range(2):
+            cats.cats_verify_layers_quantized(ctx, arr, l, l + 1, each, kv, 40)
+        assert torch.isfinite(both).all() and not torch.equal(both, x)
+        assert torch.equal(both, each) and all(torch.equal(a, b) for a, b in zip(rows, ks + vs))
+    finally:
+        torch.cuda.synchronize()
+        cats.cats_destroy(ctx)
+
+
 def test_whole_step_beside_the_bf16_step():
     """Embedding rows, 8-bit layers, LM head, acceptance and roll-back: the step of a target in 8 bits.  Its logits are near those of
     the bf16 target (8 bits a row: some per cent), and the context serves both kinds of step."""
