@@ -10,9 +10,9 @@
 struct QuantTile {
     int bm, bn, cost;   // rows, columns, cost of a round of one tile per compute unit
 };
-constexpr QuantTile QUANT_TILES[] = {{16, 16, 32},   {16, 32, 48},   {32, 32, 64},    {64, 32, 96},   {64, 48, 112},
-                                     {64, 64, 128},  {64, 96, 160},  {64, 112, 176},  {96, 96, 192},  {128, 64, 192},
-                                     {128, 96, 250}, {96, 128, 288}, {128, 128, 350}, {128, 256, 500}, {256, 256, 700}};
+constexpr QuantTile QUANT_TILES[] = {{16, 16, 32},   {16, 32, 50},    {32, 16, 48},    {32, 32, 64},   {64, 32, 96},  {64, 48, 112},
+                                     {64, 64, 128},  {64, 96, 160},   {64, 112, 176},  {96, 96, 192},  {128, 64, 192}, {128, 96, 250},
+                                     {96, 128, 288}, {128, 128, 350}, {128, 256, 500}, {256, 256, 700}};
 constexpr int N_QUANT_TILES = sizeof(QUANT_TILES) / sizeof(QUANT_TILES[0]);
 inline int quant_tile_choice(int rows, int cols, int n_cus) {
     int best = 0;

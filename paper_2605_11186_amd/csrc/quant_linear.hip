@@ -23,8 +23,9 @@ namespace {
 // Splitting k over the waves, not over workgroups, needs no scratch memory and no second launch; X and W both go through LDS because
 // then every wait is for a count of copies that is known here (a load that the compiler sees in between makes it wait for
 // more), and eight lanes copy a whole line of a row of X.
-// A ring of one step and more workgroups a compute unit beat deeper rings for all tiles but 64 x 32 (256 x 4096 x 4096, 64 x 64:
-// 9.8 against 9.9 us, 512 rows 16.2 against 18.2).
+// Two steps in a wave's ring where one tile a compute unit is all there is and its steps are small: more of the weights are under
+// way (one row, 4096 x 11008 weights from memory: 10.4 -> 8.9 us; 63 rows in tiles of 32 x 32 17.8 -> 15.6; nothing lost from the
+// cache).  One step and more workgroups a compute unit for the larger ones (64 x 64: 512 x 4096 x 4096 16.2 against 18.2 us).
 // ONCE: the weights are copied past the caches (see launch_split).
 template <int MB, int NB, int KW, int NS, bool ONCE>
 __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearArgs a, int m_tiles, int n_tiles) {
@@ -190,9 +191,10 @@ int quant_cus() {
 void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
     if (a.rows < 1) return;
     static constexpr void (*LAUNCH[])(const QuantLinearArgs&, int, hipStream_t) = {
-        launch_split<1, 1, 8, 1>, launch_split<1, 2, 8, 1>, launch_split<2, 2, 8, 1>, launch_split<4, 2, 4, 2>, launch_split<4, 3, 4, 1>,
-        launch_split<4, 4, 4, 1>, launch_split<4, 6, 4, 1>, launch_split<4, 7, 4, 1>, launch_split<6, 6, 4, 1>, launch_split<8, 4, 4, 1>,
-        launch_split<8, 6, 4, 1>, launch_split<6, 8, 4, 1>, launch_split<8, 8, 4, 1>, launch_quant_tiles_half,  launch_quant_tiles};
+        launch_split<1, 1, 8, 2>, launch_split<1, 2, 8, 1>, launch_split<2, 1, 8, 2>, launch_split<2, 2, 8, 2>, launch_split<4, 2, 4, 2>,
+        launch_split<4, 3, 4, 1>, launch_split<4, 4, 4, 1>, launch_split<4, 6, 4, 1>, launch_split<4, 7, 4, 1>, launch_split<6, 6, 4, 1>,
+        launch_split<8, 4, 4, 1>, launch_split<8, 6, 4, 1>, launch_split<6, 8, 4, 1>, launch_split<8, 8, 4, 1>, launch_quant_tiles_half,
+        launch_quant_tiles};
     static_assert(sizeof(LAUNCH) / sizeof(LAUNCH[0]) == N_QUANT_TILES, "one kernel for each tile");
     LAUNCH[quant_tile_choice(a.rows, a.cols, n_cus)](a, n_cus, st);
 }
