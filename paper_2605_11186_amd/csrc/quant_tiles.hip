@@ -1,8 +1,8 @@
 // The product of 8-bit integers for many rows (prompts): bound by the matrix instructions.  4096 x 4096 x 11008 takes 139 us =
 // 2.65 Pop/s on tiles of 256 x 256 (the library's product of 8-bit integers 147 to 152 us; the bare instruction, fed from registers,
-// reaches 4.0 Pop/s at the clock that this power allows).  The matrix units are busy two thirds of the time; a quarter of the
-// waves' time goes into waiting for operands and for each other: timing copies without the weight loads take 13 % less, without
-// the copies of X 12 % less.
+// reaches 4.0 Pop/s at the clock that this power allows).  The matrix units are busy two thirds of the time; what they wait for
+// is operands from the L2: timing copies without the weight loads take 13 % less, without the copies of X 12 %, without the step's
+// barrier or the reads from LDS as long.  With operands of zeros it takes 130 us: the rest of the way is the clock.
 #include <algorithm>
 #include <type_traits>
 
