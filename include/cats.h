@@ -46,7 +46,7 @@ extern "C" {
 typedef enum {
     CATS_OK = 0,
     CATS_EINVAL = -1,    /* null pointer, bad shape, malformed tree, token out of range */
-    CATS_ECAPACITY = -2, /* ctx_len + T exceeds max_ctx, or a tree exceeds its arrays       */
+    CATS_ECAPACITY = -2, /* ctx_len + T exceeds max_ctx, a tree its arrays, a length its limit */
     CATS_ESTATE = -3,    /* no tree has been set                                         */
     CATS_EHIP = -4       /* a HIP runtime call failed                                    */
 } cats_status;

@@ -83,14 +83,15 @@ struct cats_ctx {
     hipEvent_t prof_ev[2 * CATS_PROF_MAX];
 };
 
-namespace {
+static thread_local hipError_t g_last_hip = hipSuccess;
 
-thread_local hipError_t g_last_hip = hipSuccess;
-
-inline int hip_fail(hipError_t e) {
+int hip_fail(hipError_t e) {
     g_last_hip = e;
     return CATS_EHIP;
 }
+
+namespace {
+
 #define HIP_TRY(expr)                                  \
     do {                                               \
         hipError_t e_ = (expr);                        \
@@ -1502,10 +1503,10 @@ const char* cats_gemm_kernel_name(void) { return "cats_gemm_skinny_bf16"; }
 const char* cats_strerror(int status) {
     switch (status) {
         case CATS_OK: return "ok";
-        case CATS_EINVAL: return "invalid argument (null pointer, bad shape, malformed tree or token out of range)";
+        case CATS_EINVAL: return "invalid argument (null or misaligned pointer, bad shape or type, malformed tree or token out of range)";
         case CATS_ECAPACITY:
-            return "capacity exceeded (ctx_len + tree size > max_ctx, more nodes than the arrays hold, or a shape too "
-                   "large for the fixed scratch of the no-allocation entry point)";
+            return "capacity exceeded (ctx_len + tree size > max_ctx, more nodes than the arrays hold, a shape too "
+                   "large for the fixed scratch of the no-allocation entry point, or a length above an operator's limit)";
         case CATS_ESTATE: return "no tree has been set on this context";
         case CATS_EHIP: return hipGetErrorString(g_last_hip);
         default: return "unknown status";

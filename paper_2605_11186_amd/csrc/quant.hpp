@@ -4,6 +4,14 @@
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
+// CATS_EHIP; cats_strerror then gives the text of e.
+int hip_fail(hipError_t e);
+// The status behind a launch.
+inline int launch_status() {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? CATS_OK : hip_fail(e);
+}
+
 // ---------------------------------------------------------------- rows in 8 bits
 // What a row is before it is quantised: ROWS_PLAIN the source row; ROWS_NORM (src + delta) normalised and
 // times gain; ROWS_SWIGLU silu(first half of the source row) * second half.

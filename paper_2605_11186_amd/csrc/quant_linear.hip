@@ -173,17 +173,20 @@ int64_t frags_of(int32_t rows, int32_t cols) {
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
-// Compute units of the current device (0: it could not be asked).
-int quant_cus() {
+// Compute units of the current device.
+hipError_t quant_cus(int& n) {
     constexpr int MAX_DEVICES = 64;
     static std::atomic<int> known[MAX_DEVICES];   // zero: not asked yet
-    int dev = 0, n = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) return 0;
-    n = known[dev].load(std::memory_order_relaxed);
-    if (n) return n;
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return 0;
-    known[dev].store(n, std::memory_order_relaxed);
-    return n;
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const bool keep = dev >= 0 && dev < MAX_DEVICES;
+    n = keep ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (n) return hipSuccess;
+    e = hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev);
+    if (e == hipSuccess && n < 1) e = hipErrorInvalidDevice;
+    if (e == hipSuccess && keep) known[dev].store(n, std::memory_order_relaxed);
+    return e;
 }
 
 }  // namespace
@@ -212,7 +215,7 @@ int cats_pack_quantized_matrix(const int8_t* src, int64_t src_ld, int32_t rows, 
     const unsigned groups = static_cast<unsigned>(std::min<int64_t>((frags + 3) / 4, 1 << 16));
     hipLaunchKernelGGL(cats_quant_pack, dim3(groups), dim3(256), 0, static_cast<hipStream_t>(stream), src, src_ld, dst, rows, cols,
                        qpack_chunks(cols), frags, aligned16(src) && src_ld % 16 == 0);
-    return hipGetLastError() == hipSuccess ? CATS_OK : CATS_EHIP;
+    return launch_status();
 }
 
 int cats_quantized_linear(const int8_t* x, int64_t x_ld, const float* x_scale, const int8_t* w_packed, const float* w_scale,
@@ -228,8 +231,12 @@ int cats_quantized_linear(const int8_t* x, int64_t x_ld, const float* x_scale, c
         static_cast<int64_t>(rows) * cols > (int64_t{1} << 33))   // threads of a launch: fewer than 2^32
         return CATS_ECAPACITY;
     if (rows == 0) return CATS_OK;
-    const int n_cus = quant_cus();
-    if (!n_cus) return CATS_EHIP;
+    int n_cus = 0;
+    const hipError_t e = quant_cus(n_cus);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();   // the next launch is not to blame for it
+        return hip_fail(e);
+    }
     QuantLinearArgs a{};
     a.x = x;
     a.x_ld = x_ld;
@@ -244,7 +251,7 @@ int cats_quantized_linear(const int8_t* x, int64_t x_ld, const float* x_scale, c
     a.inner = inner;
     a.chunks = qpack_chunks(inner);
     launch_quant_linear(a, n_cus, static_cast<hipStream_t>(stream));
-    return hipGetLastError() == hipSuccess ? CATS_OK : CATS_EHIP;
+    return launch_status();
 }
 
 }  // extern "C"

@@ -284,7 +284,7 @@ int check_rows(int32_t rows, int32_t cols, const int8_t* q, int64_t q_ld, const 
 int enqueue(const QuantRowsArgs& a, int kind, void* stream) {
     if (a.rows == 0) return CATS_OK;
     launch_quant_rows(a, kind, static_cast<hipStream_t>(stream));
-    return hipGetLastError() == hipSuccess ? CATS_OK : CATS_EHIP;
+    return launch_status();
 }
 
 }  // namespace

@@ -109,3 +109,12 @@ def test_binding_refuses_what_does_not_fit():
         with pytest.raises(cats.CatsError) as e:
             f()
         assert e.value.status == cats.CATS_EINVAL
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="on a device these calls would run")
+@pytest.mark.parametrize("name,base", [("cats_quantize_rows", QUANTIZE), ("cats_rmsnorm_quantize", NORM), ("cats_swiglu_quantize", SWIGLU),
+                                       ("cats_pack_quantized_matrix", PACK), ("cats_quantized_linear", LINEAR)])
+def test_a_failure_of_the_device_has_its_text(name, base):
+    lib = cats.library()
+    assert call(name, base) == cats.CATS_EHIP
+    assert lib.cats_strerror(cats.CATS_EHIP) == b"no ROCm-capable device is detected"
