@@ -15,23 +15,26 @@ namespace {
 // weights are the first operand: a lane's four results are neighbouring columns of y.
 
 // From one row to some hundreds.  A workgroup owns a tile of 16 MB rows and 16 NB columns; its KW waves take turns at the steps
-// of 128 values of k and add up their sums through LDS at the end.  Each wave keeps NS of its steps in a ring of LDS that nobody
-// else touches: it waits for its own copies only, reads a step's fragments, sends for the step that takes their place, and
-// multiplies; there is no barrier before the sums meet.
+// of 128 values of k and add up their sums through LDS at the end.  Each wave keeps the rows of NS and the weights of NW of its steps
+// in rings of LDS that nobody else touches: it waits for its own copies only, reads a step's fragments, sends for what takes their
+// place, and multiplies; there is no barrier before the sums meet.
 // Bound by the operands' way into the compute unit: with few rows the weights' from memory (22016 x 4096 weights: 14.7 us with
 // one row = 6.1 TB/s, 19.5 with 63 rows), with more the rows' and the weights' from the L2 (see quant_choice.hpp).
 // Splitting k over the waves, not over workgroups, needs no scratch memory and no second launch; X and W both go through LDS because
 // then every wait is for a count of copies that is known here (a load that the compiler sees in between makes it wait for
 // more), and eight lanes copy a whole line of a row of X.
-// Two steps in a wave's ring where one tile a compute unit is all there is and its steps are small: more of the weights are under
-// way (one row, 4096 x 11008 weights from memory: 10.4 -> 8.9 us; 63 rows in tiles of 32 x 32 17.8 -> 15.6; nothing lost from the
-// cache).  One step and more workgroups a compute unit for the larger ones (64 x 64: 512 x 4096 x 4096 16.2 against 18.2 us).
+// Two steps in a wave's rings where one tile a compute unit is all there is and its steps are small: more of the weights are under
+// way (one row, 4096 x 11008 weights from memory: 10.4 -> 8.9 us; nothing lost from the cache); of the weights alone in the middle
+// sizes (63 x 8192 x 11008 from memory 26.2 -> 23.1 us).  One step and more workgroups a compute unit for the larger ones (64 x 64:
+// 512 x 4096 x 4096 18.1 against 18.6 us with two steps of weights), unless the weights come past the caches.
+// A compute unit takes in rows at 63 GB/s from the L2 and weights at 22 from memory, and the two times add up: its requests come
+// back in order.  So 128 x 15360 x 5120 with weights from memory takes 25 us, 64 rows 18.7, one 14.
 // ONCE: the weights are copied past the caches (see launch_split).
-template <int MB, int NB, int KW, int NS, bool ONCE>
+template <int MB, int NB, int KW, int NS, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearArgs a, int m_tiles, int n_tiles) {
-    constexpr int COPIES = 2 * (MB + NB), STEP = COPIES * 1024;   // of a step: copies of 1 KB, bytes
-    static_assert(NS <= 2 && (NS - 1) * COPIES < 64, "counts of the waits");
-    constexpr int RING = KW * NS * STEP;
+    constexpr int UNDER_WAY = (NS - 1) * 2 * MB + (NW - 1) * 2 * NB;   // copies of 1 KB behind a step's own
+    static_assert(NS <= 2 && NW - NS <= 1 && NW >= NS && UNDER_WAY < 64, "counts of the waits");
+    constexpr int OWN = (NS * MB + NW * NB) * 2048, RING = KW * OWN;
     // the waves' sums meet in parts of PB row blocks that fit where the ring was
     constexpr int PB = KW * MB * NB * 1024 <= RING ? MB : MB / 2;
     static_assert(KW * PB * NB * 1024 <= RING && MB % PB == 0, "a part of the sums fits the ring");
@@ -58,17 +61,21 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
     const int8_t* wp[NB];
 #pragma unroll
     for (int j = 0; j < NB; ++j) wp[j] = a.w + static_cast<int64_t>(min(nt * NB + j, n_rb - 1)) * a.chunks * QPACK_FRAG;
-    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&s_lds[0])) + wave * NS * STEP;
-    auto fetch = [&](int i, int slot) {   // the i-th of this wave's steps
-        const int s = wave + i * KW, k = min(s * 128 + piece, k_last);
-        const uint32_t to = lds0 + slot * STEP;
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&s_lds[0])) + wave * OWN;
+    auto fetch_w = [&](int i, int slot) {   // for the i-th of this wave's steps
+        const int s = wave + i * KW;
+        const uint32_t to = lds0 + slot * NB * 2048;
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             copy_to_lds<ONCE>(wp[j] + s * 2048, lane * 16, to + j * 2048);
             copy_to_lds<ONCE>(wp[j] + s * 2048 + 1024, lane * 16, to + j * 2048 + 1024);
         }
+    };
+    auto fetch_x = [&](int i, int slot) {
+        const int k = min((wave + i * KW) * 128 + piece, k_last);
+        const uint32_t to = lds0 + (NW * NB + slot * MB) * 2048;
 #pragma unroll
-        for (int p = 0; p < 2 * MB; ++p) copy_to_lds(x0, xo[p] + k, to + NB * 2048 + p * 1024);
+        for (int p = 0; p < 2 * MB; ++p) copy_to_lds(x0, xo[p] + k, to + p * 1024);
     };
     i32x4 acc[MB][NB];
 #pragma unroll
@@ -77,28 +84,33 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
         for (int j = 0; j < NB; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
     const int r = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int i = 0; i < NS; ++i)
-        if (i < mine) fetch(i, i);
-    int slot = 0;
+    for (int i = 0; i < NW; ++i) {
+        if (i < mine) fetch_w(i, i);
+        if (i < NS && i < mine) fetch_x(i, i);
+    }
+    int slot = 0, w_slot = 0;
     for (int i = 0; i < mine; ++i) {
-        // this step's copies; of the NS - 1 behind it all are under way until the last ones
-        if (mine - 1 - i >= NS - 1)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 1) * COPIES) : "memory");
+        // this step's copies; all behind them are under way until the last steps
+        if (mine - 1 - i >= NW - 1)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(UNDER_WAY) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        const int8_t* from = &s_lds[0] + (wave * NS + slot) * STEP;
+        const int8_t* w_from = &s_lds[0] + wave * OWN + w_slot * NB * 2048;
+        const int8_t* x_from = &s_lds[0] + wave * OWN + (NW * NB + slot * MB) * 2048;
         i32x4 w[2][NB], x[2][MB];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int j = 0; j < NB; ++j) w[h][j] = *reinterpret_cast<const i32x4*>(from + j * 2048 + h * 1024 + lane * 16);
+            for (int j = 0; j < NB; ++j) w[h][j] = *reinterpret_cast<const i32x4*>(w_from + j * 2048 + h * 1024 + lane * 16);
 #pragma unroll
             for (int b = 0; b < MB; ++b)
-                x[h][b] = *reinterpret_cast<const i32x4*>(from + NB * 2048 + (b * 16 + r) * 128 + ((4 * h + g) ^ (r & 7)) * 16);
+                x[h][b] = *reinterpret_cast<const i32x4*>(x_from + (b * 16 + r) * 128 + ((4 * h + g) ^ (r & 7)) * 16);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the fragments are in registers: their place is free
-        if (i + NS < mine) fetch(i + NS, slot);
+        if (i + NS < mine) fetch_x(i + NS, slot);
+        if (i + NW < mine) fetch_w(i + NW, w_slot);
         slot = slot == NS - 1 ? 0 : slot + 1;
+        w_slot = w_slot == NW - 1 ? 0 : w_slot + 1;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -134,11 +146,13 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
 // 22.8 -> 20.1, one row 17.2 -> 15.7, with three (270 MB) 19.9 -> 19.6; 63 x 4096 x 11008, forty in turn, 17.3 -> 15.5.  Smaller
 // ones may be of a model that the cache holds: three of 4096 x 11008 in turn take 8.4 us with one row, past the caches 9.8.
 constexpr int64_t CACHE_BYTES = int64_t{256} << 20;
-template <int MB, int NB, int KW, int NS>
+template <int MB, int NB, int KW, int NS, int NW>
 void launch_split(const QuantLinearArgs& a, int, hipStream_t st) {
     const int m_tiles = (a.rows + 16 * MB - 1) / (16 * MB), n_tiles = (a.cols + 16 * NB - 1) / (16 * NB);
     const bool once = a.cold ? m_tiles <= (MB <= 2 ? 2 : 1) : m_tiles == 1 && static_cast<int64_t>(a.cols) * a.inner >= CACHE_BYTES / 3;
-    hipLaunchKernelGGL((once ? cats_quant_linear_split<MB, NB, KW, NS, true> : cats_quant_linear_split<MB, NB, KW, NS, false>),
+    // weights that come past the caches, one step further ahead where the LDS holds it (63 x 27648 x 5120 30.0 -> 28.2 us)
+    constexpr int ONCE_NW = NW == 1 && MB >= 4 && (MB + 2 * NB) * 2048 * KW < 156 * 1024 ? 2 : NW;
+    hipLaunchKernelGGL((once ? cats_quant_linear_split<MB, NB, KW, NS, ONCE_NW, true> : cats_quant_linear_split<MB, NB, KW, NS, NW, false>),
                        dim3(static_cast<unsigned>(m_tiles) * n_tiles), dim3(64 * KW), 0, st, a, m_tiles, n_tiles);
 }
 
@@ -194,10 +208,13 @@ hipError_t quant_cus(int& n) {
 void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
     if (a.rows < 1) return;
     static constexpr void (*LAUNCH[])(const QuantLinearArgs&, int, hipStream_t) = {
-        launch_split<1, 1, 8, 2>, launch_split<1, 2, 8, 1>, launch_split<2, 1, 8, 2>, launch_split<2, 2, 8, 2>, launch_split<4, 2, 4, 2>,
-        launch_split<4, 3, 4, 1>, launch_split<4, 4, 4, 1>, launch_split<4, 6, 4, 1>, launch_split<4, 7, 4, 1>, launch_split<6, 6, 4, 1>,
-        launch_split<8, 4, 4, 1>, launch_split<8, 6, 4, 1>, launch_split<6, 8, 4, 1>, launch_split<8, 8, 4, 1>, launch_quant_tiles_half,
-        launch_quant_tiles};
+        launch_split<1, 1, 8, 2, 2>, launch_split<1, 2, 8, 1, 1>, launch_split<1, 3, 8, 1, 1>, launch_split<2, 1, 8, 2, 2>,
+        launch_split<2, 2, 8, 2, 2>, launch_split<2, 3, 4, 1, 2>, launch_split<2, 4, 4, 1, 2>, launch_split<2, 6, 4, 1, 2>,
+        launch_split<2, 7, 4, 1, 2>, launch_split<2, 8, 4, 1, 2>, launch_split<4, 2, 4, 1, 2>, launch_split<4, 3, 4, 1, 1>,
+        launch_split<4, 4, 4, 1, 1>, launch_split<4, 6, 4, 1, 1>, launch_split<4, 7, 4, 1, 1>, launch_split<4, 8, 4, 1, 1>,
+        launch_split<6, 6, 4, 1, 1>, launch_split<8, 4, 4, 1, 1>, launch_split<8, 6, 4, 1, 1>, launch_split<6, 8, 4, 1, 1>,
+        launch_split<8, 7, 4, 1, 1>, launch_split<8, 8, 4, 1, 1>,
+        launch_quant_tiles_half, launch_quant_tiles};
     static_assert(sizeof(LAUNCH) / sizeof(LAUNCH[0]) == N_QUANT_TILES, "one kernel for each tile");
     LAUNCH[quant_tile_choice(a.rows, a.cols, n_cus)](a, n_cus, st);
 }

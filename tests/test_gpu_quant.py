@@ -256,9 +256,11 @@ def test_linear(rows, cols, inner, dtype):
 
 
 # one size for each tile that a product is cut into on 256 compute units (tests/test_quant_choice.py), none of them whole
-TILE_SIZES = {(16, 16): (13, 1003), (16, 32): (9, 4107), (32, 16): (27, 4091), (32, 32): (30, 4107), (64, 32): (62, 4107), (64, 48): (57, 10007),
-              (64, 64): (254, 4077), (64, 96): (61, 21001), (64, 112): (61, 27001), (96, 96): (95, 21001), (128, 64): (509, 4077),
-              (128, 96): (125, 21001), (96, 128): (763, 4077), (128, 128): (1021, 4077), (128, 256): (2001, 4077), (256, 256): (4001, 4077)}
+TILE_SIZES = {(16, 16): (13, 1003), (16, 32): (9, 4107), (16, 48): (9, 12001), (32, 16): (27, 4091), (32, 32): (30, 4107),
+              (32, 48): (29, 12001), (32, 64): (31, 15307), (32, 96): (29, 21001), (32, 112): (27, 27001), (32, 128): (31, 32001),
+              (64, 32): (62, 8001), (64, 48): (57, 10007), (64, 64): (254, 4077), (64, 96): (61, 21001), (64, 112): (61, 27001),
+              (64, 128): (63, 32001), (96, 96): (95, 21001), (128, 64): (509, 4077), (128, 96): (125, 21001), (96, 128): (763, 4077),
+              (128, 112): (125, 27001), (128, 128): (1021, 4077), (128, 256): (2001, 4077), (256, 256): (4001, 4077)}
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
@@ -269,10 +271,12 @@ def test_linear_every_tile(tile, inner, dtype):
 
 
 # few rows and some hundred megabytes of weights, which pass the caches by: one size for each tile that takes them all in one row tile
-ONCE_SIZES = {(16, 16): (9, 4077, 22001), (16, 32): (3, 22001, 4099), (32, 16): (31, 4077, 22001), (32, 32): (29, 4107, 22001), (64, 32): (59, 4107, 22001),
-              (64, 48): (57, 10007, 9003), (64, 64): (61, 15307, 6003), (64, 96): (61, 21001, 4301), (64, 112): (61, 27001, 3401),
+ONCE_SIZES = {(16, 16): (9, 4077, 22001), (16, 32): (3, 8177, 11203), (16, 48): (3, 22001, 4099), (32, 16): (31, 4077, 22001),
+              (32, 32): (29, 4107, 22001), (32, 48): (29, 12001, 7501), (32, 64): (31, 15307, 6003), (32, 96): (29, 21001, 4301),
+              (32, 112): (27, 27001, 3401), (32, 128): (31, 32001, 2807), (64, 32): (59, 8001, 11203), (64, 48): (57, 10007, 9003),
+              (64, 64): (61, 15307, 6003), (64, 96): (61, 21001, 4301), (64, 112): (61, 27001, 3401), (64, 128): (63, 32001, 2807),
               (96, 96): (95, 21001, 4301), (128, 64): (125, 15307, 6003), (128, 96): (125, 21001, 4301), (96, 128): (95, 32001, 2807),
-              (128, 128): (125, 27001, 3401)}
+              (128, 112): (125, 27001, 3401), (128, 128): (125, 32001, 2807)}
 
 
 @pytest.mark.parametrize("tile", sorted(ONCE_SIZES))
