@@ -14,10 +14,11 @@ inline int launch_status() {
 
 // ---------------------------------------------------------------- rows in 8 bits
 // What a row is before it is quantised: ROWS_PLAIN the source row; ROWS_NORM (src + delta) normalised and
-// times gain; ROWS_SWIGLU silu(first half of the source row) * second half.
-enum { ROWS_PLAIN = 0, ROWS_NORM = 1, ROWS_SWIGLU = 2 };
+// times gain; ROWS_SWIGLU silu(first half of the source row) * second half; ROWS_MERGED the single row that the chunks of a
+// single query's attention make (see DecodeAttnArgs), rounded to bf16.
+enum { ROWS_PLAIN = 0, ROWS_NORM = 1, ROWS_SWIGLU = 2, ROWS_MERGED = 3 };
 struct QuantRowsArgs {
-    const void* src;       // float32 or bf16 (ROWS_NORM: float32)
+    const void* src;       // float32 or bf16 (ROWS_NORM: float32; ROWS_MERGED: DecodeAttnArgs.po)
     const void* delta;     // ROWS_NORM, optional
     const bf16_t* gain;    // ROWS_NORM: [cols]
     float* x_out;          // ROWS_NORM with delta: the updated rows (may be src)
@@ -27,6 +28,8 @@ struct QuantRowsArgs {
     int rows, cols;
     float eps;
     int src_type, delta_type;   // CATS_F32, CATS_BF16
+    const float* ml;       // ROWS_MERGED: DecodeAttnArgs.pml
+    int n_chunks, head_dim;
 };
 // kind: ROWS_*.  Nothing is enqueued for no rows.
 void launch_quant_rows(const QuantRowsArgs& a, int kind, hipStream_t st);

@@ -1,6 +1,6 @@
 // Rows in 8-bit integers with one scale each, and the steps of a decoder layer that end in such rows:
 //   q = rint(127 v / max|v|) (ties to even),  scale = max|v| / 127 (at least 2^-126)
-// for v = a source row, v = rmsnorm(x + delta) * gain, or v = silu(gate) * up.
+// for v = a source row, v = rmsnorm(x + delta) * gain, v = silu(gate) * up, or v = the merged chunks of a single query's attention.
 //
 // One pass: a row is read once, held in the registers of the threads that share it (8 values a thread and piece)
 // until its maximum (for the norm its sum of squares first) is known, and written as bytes.  There is no matrix work and no more
@@ -84,6 +84,65 @@ __device__ __forceinline__ Raw<T, VEC> load8(const T* row, int tid, int j, int c
     return r;
 }
 
+// ROWS_MERGED: columns k .. k + 7 belong to head k / head_dim, whose chunks are merged in index order, CH chunks' loads in flight
+// at a time, rescaled to the running maximum between groups.  One workgroup reads it all at some 60 GB/s (32 heads of 128: 16 KB
+// a chunk); the row's maximum leaves no work for more.
+template <int TPR, int NC>
+__device__ __forceinline__ void merge_chunks(const QuantRowsArgs& a, int tid, float (&v)[NC][8]) {
+    constexpr int CH = 8;
+    const float* po[NC];
+    const float* ml[NC];
+    float den[NC], top[NC];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+        const int k = min(place<TPR, true>(tid, j, 0), a.cols - 8), h = k / a.head_dim;
+        po[j] = static_cast<const float*>(a.src) + static_cast<size_t>(h) * a.n_chunks * a.head_dim + (k - h * a.head_dim);
+        ml[j] = a.ml + static_cast<size_t>(h) * a.n_chunks * 2;
+        den[j] = 0.f;
+        top[j] = -1e30f;   // where a chunk's maximum starts, too
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[j][e] = 0.f;
+    }
+    for (int c0 = 0; c0 < a.n_chunks; c0 += CH) {
+        f32x4 x[NC][CH][2];
+        float mc[NC][CH], lc[NC][CH];
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int c = min(c0 + i, a.n_chunks - 1);   // (clamped repeats do not change the maximum and do not count)
+                mc[j][i] = ml[j][2 * c];
+                lc[j][i] = ml[j][2 * c + 1];
+                const f32x4* p = reinterpret_cast<const f32x4*>(po[j] + static_cast<size_t>(c) * a.head_dim);
+                x[j][i][0] = p[0];
+                x[j][i][1] = p[1];
+            }
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            float most = top[j];
+#pragma unroll
+            for (int i = 0; i < CH; ++i) most = fmaxf(most, mc[j][i]);
+            const float before = __builtin_amdgcn_exp2f(top[j] - most);
+            top[j] = most;
+            den[j] *= before;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[j][e] *= before;
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+                if (c0 + i < a.n_chunks) {
+                    const float w = __builtin_amdgcn_exp2f(mc[j][i] - most);
+                    den[j] = fmaf(w, lc[j][i], den[j]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[j][e] = fmaf(w, x[j][i][e >> 2][e & 3], v[j][e]);
+                }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[j][e] *= 1.f / den[j];
+}
+
 // TPR threads share a row (64: four rows a workgroup), NC pieces of 8 values each.  T: type of the source.
 // D: type of delta (none_t: none).
 template <int KIND, class T, class D, int TPR, int NC, bool VEC>
@@ -102,7 +161,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
     bool in[NC][VEC ? 1 : 8];
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-        r0[j] = load8<T, TPR, VEC>(src, tid, j, cols);
+        if constexpr (KIND != ROWS_MERGED) r0[j] = load8<T, TPR, VEC>(src, tid, j, cols);
 #pragma unroll
         for (int e = 0; e < (VEC ? 1 : 8); ++e) in[j][e] = place<TPR, VEC>(tid, j, e) < cols;
     }
@@ -111,6 +170,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
         for (int j = 0; j < NC; ++j)
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[j][e] = in[j][VEC ? 0 : e] ? r0[j].get(e) : 0.f;
+    } else if constexpr (KIND == ROWS_MERGED) {
+        merge_chunks<TPR, NC>(a, tid, v);
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[j][e] = in[j][0] ? bf2f(f2bf(v[j][e])) : 0.f;
     } else if constexpr (KIND == ROWS_SWIGLU) {
         Raw<T, VEC> r1[NC];
 #pragma unroll
@@ -199,13 +264,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
     if (tid == 0) a.scale[t] = finite ? most / 127.f : NAN;
     // y + 1.5 * 2^23: the sum's last bits are the whole number nearest to y in two's complement (ties to even)
     constexpr float WHOLE = 12582912.f;
-    // ROWS_PLAIN: y = 127 v / most as a correctly rounded quotient (by one correction), so that ties, which are common among bf16
+    // ROWS_PLAIN, ROWS_MERGED: y = 127 v / most as a correctly rounded quotient (by one correction), so that ties, which are common among bf16
     // values, are seen: by the power of two p, most p lies in [1, 4) and no product leaves the range.  Computed rows have no ties
     // worth the three instructions a value.
     const float p = __uint_as_float(max(0x7F000000u - (__float_as_uint(most) & 0x7F800000u), 0x00800000u));
-    const float den = KIND == ROWS_PLAIN ? most * p : most, mul = KIND == ROWS_PLAIN ? 127.f * p : 127.f / most, rden = 1.f / den;
+    constexpr bool TIES = KIND == ROWS_PLAIN || KIND == ROWS_MERGED;
+    const float den = TIES ? most * p : most, mul = TIES ? 127.f * p : 127.f / most, rden = 1.f / den;
     auto whole = [&](float v) {
-        if constexpr (KIND == ROWS_PLAIN) {
+        if constexpr (TIES) {
             const float z = v * mul, y = z * rden;
             return __float_as_uint(fmaf(fmaf(-y, den, z), rden, y) + WHOLE);
         } else {
@@ -291,6 +357,13 @@ int enqueue(const QuantRowsArgs& a, int kind, void* stream) {
 
 void launch_quant_rows(const QuantRowsArgs& a, int kind, hipStream_t st) {
     if (a.rows < 1) return;
+    if (kind == ROWS_MERGED) {
+        const int pieces = a.cols / 8;
+        if (pieces <= 64) return launch<ROWS_MERGED, float, none_t, 64, 1, true>(a, st);
+        if (pieces <= 256) return launch<ROWS_MERGED, float, none_t, 256, 1, true>(a, st);
+        if (pieces <= 512) return launch<ROWS_MERGED, float, none_t, 512, 1, true>(a, st);
+        return launch<ROWS_MERGED, float, none_t, 1024, 1, true>(a, st);
+    }
     const bool f32 = a.src_type == CATS_F32;
     if (kind == ROWS_PLAIN)
         return f32 ? by_alignment<ROWS_PLAIN, float, none_t>(a, st) : by_alignment<ROWS_PLAIN, bf16_t, none_t>(a, st);

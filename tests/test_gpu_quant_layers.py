@@ -142,6 +142,59 @@ def test_layers(model, nodes, ctx_len):
     assert torch.equal(again, hidden)
 
 
+@pytest.mark.parametrize("ctx_len", [127, 128, 1029, 2100, 4400])   # 1, 1, 9, 17 and 18 chunks of keys
+@pytest.mark.parametrize("dims", [synth.TINY, WIDE], ids=["heads64", "heads128"])
+def test_a_single_node_behind_long_contexts(dims, ctx_len):
+    model = Model(dims, 3, max_ctx=4480, max_tree=1)
+    try:
+        kr, vr, ks, vs = model.caches(5, ctx_len)
+        x = synth.random_hidden(dims, 6, 1)
+        hidden = torch.from_numpy(np.asarray(x, dtype=np.float32)).cuda()
+        cats.cats_set_tree(model.ctx, np.zeros(1, np.int32), *tree_of(1, 1))
+        cats.cats_verify_layers_quantized(model.ctx, model.arr, 0, dims.n_layers, hidden, cats.kv_array(ks, vs), ctx_len)
+        torch.cuda.synchronize()
+        want, new = reference(dims, np.asarray(x, dtype=np.float64), model.ref, kr, vr, ctx_len, *tree_of(1, 1))
+        e = [rel_err(hidden.cpu().numpy(), want)]
+        for l in range(dims.n_layers):
+            k, v = cats.kv_to_rows(ks[l], vs[l], ctx_len + 1)
+            assert np.array_equal(bf16_to_f32_np(k[:ctx_len]), kr[l].astype(np.float32))
+            e += [rel_err(bf16_to_f32_np(k[ctx_len:]), new[l][0]), rel_err(bf16_to_f32_np(v[ctx_len:]), new[l][1])]
+            assert torch.isnan(ks[l][:, ctx_len + 1:]).all() and torch.isnan(vs[l][:, :, ctx_len + 1:]).all()
+        assert max(e) <= REL_TOL
+    finally:
+        model.close()
+
+
+@pytest.mark.parametrize("hidden,ctx_len", [(2048, 700), (4096, 1500), (5120, 1000), (8192, 300), (8192, 1530), (8192, 1700)])
+def test_a_single_node_as_the_root_of_two(hidden, ctx_len):
+    """A single node's attention has kernels of its own up to a number of chunks: the root of a tree sees the same rows."""
+    heads, ffn = hidden // 128, 1024
+    gen = torch.Generator(device="cuda").manual_seed(23)
+
+    def random(*shape, by=1.0):
+        return torch.empty(*shape, device="cuda").normal_(0, by, generator=gen).to(torch.bfloat16)
+
+    one = torch.ones(hidden, dtype=torch.bfloat16, device="cuda")
+    layer = cats.quantize_layer(dict(wq=random(hidden, hidden, by=0.02), wk=random(hidden, hidden, by=0.02), wv=random(hidden, hidden, by=0.02),
+                                     wo=random(hidden, hidden, by=0.02), w_gate=random(ffn, hidden, by=0.02), w_up=random(ffn, hidden, by=0.02),
+                                     w_down=random(hidden, ffn, by=0.02), g_attn=one, g_ffn=one))
+    ctx = cats.cats_create(cats.ModelDesc(1, hidden, heads, 128, ffn, 1000, 2048, 2, 1e-6, 1e4, 0))
+    try:
+        k0, v0 = random(heads, 2048, 128), random(heads, 128, 2048)
+        x = torch.empty(2, hidden, device="cuda").normal_(generator=gen)
+        rows = []
+        for nodes in (1, 2):
+            k, v, h = k0.clone(), v0.clone(), x[:nodes].clone()
+            cats.cats_set_tree(ctx, np.zeros(nodes, np.int32), np.asarray([-1, 0][:nodes], np.int32), np.arange(nodes, dtype=np.int32))
+            cats.cats_verify_layers_quantized(ctx, cats.quantized_layer_array([layer]), 0, 1, h, cats.kv_array([k], [v]), ctx_len)
+            torch.cuda.synchronize()
+            rows.append([t.float().cpu().numpy() for t in (h[0] - x[0], k[:, ctx_len], v[:, :, ctx_len])])
+        assert max(rel_err(a, b) for a, b in zip(*rows)) <= REL_TOL
+    finally:
+        torch.cuda.synchronize()
+        cats.cats_destroy(ctx)
+
+
 @pytest.mark.parametrize("nodes", [1, 20, 63, 128])
 def test_a_call_whose_weights_pass_the_caches(nodes):
     """Two layers of 202 MB of weights in one call (past the caches) and one after the other (through them): the same bits."""
