@@ -9,6 +9,7 @@
 
 #include "common.hpp"
 #include "quant.hpp"
+#include "quant_choice.hpp"
 
 constexpr int CATS_PROF_MAX = 1024;  // GEMM launches that can be timed between two reads
 
@@ -484,7 +485,7 @@ void finish_row(cats_ctx* c, float* dst, const void* gain, hipStream_t st) {
 }
 
 // ---- layers in 8 bits.  Rows in front of a product lie in c->xn (hidden columns) or c->hact (ffn), with their scales in
-// c->qscale; every product leaves float32 rows in c->part.
+// c->qscale; every product leaves float32 rows in c->part, the output and down products in up to QUANT_MAX_PIECES pieces.
 QuantRowsArgs quant_rows(const cats_ctx* c, const void* src, int64_t src_ld, int cols, void* q) {
     QuantRowsArgs a{};
     a.src = src;
@@ -497,11 +498,12 @@ QuantRowsArgs quant_rows(const cats_ctx* c, const void* src, int64_t src_ld, int
     a.scale = c->qscale;
     return a;
 }
-// c->xn = rmsnorm(x + delta) * gain in 8 bits, x += delta; delta: the rows in c->part, or none
-void enqueue_norm_quantized(cats_ctx* c, float* x, bool delta, const void* gain, hipStream_t st) {
+// c->xn = rmsnorm(x + delta) * gain in 8 bits, x += delta; delta: that many pieces of rows in c->part, which add up to it
+void enqueue_norm_quantized(cats_ctx* c, float* x, int delta, const void* gain, hipStream_t st) {
     const int H = c->d.hidden;
     QuantRowsArgs a = quant_rows(c, x, H, H, c->xn);
     a.delta = delta ? c->part : nullptr;
+    a.delta_pieces = delta;
     a.delta_type = CATS_F32;
     a.delta_ld = H;
     a.gain = static_cast<const bf16_t*>(gain);
@@ -510,8 +512,14 @@ void enqueue_norm_quantized(cats_ctx* c, float* x, bool delta, const void* gain,
     a.x_out_ld = H;
     launch_quant_rows(a, ROWS_NORM, st);
 }
-void enqueue_linear_quantized(cats_ctx* c, const void* q, int inner, const int8_t* w, const float* w_scale, int cols, bool cold,
-                              hipStream_t st) {
+// The plan of a product that lies in c->part as this many pieces of all its columns.
+GemmPlan whole_pieces_plan(int cols, int pieces) {
+    const int items = (cols + 127) / 128 * pieces;
+    return GemmPlan{128, GEMM_KC, pieces, items, items, 1, make_fast_div(pieces), make_fast_div(items), make_fast_div(items)};
+}
+// Returns the pieces in c->part whose sum the product is: up to max_pieces.
+int enqueue_linear_quantized(cats_ctx* c, const void* q, int inner, const int8_t* w, const float* w_scale, int cols, int max_pieces,
+                             bool cold, hipStream_t st) {
     QuantLinearArgs a{};
     a.x = static_cast<const int8_t*>(q);
     a.x_ld = inner;
@@ -526,21 +534,25 @@ void enqueue_linear_quantized(cats_ctx* c, const void* q, int inner, const int8_
     a.inner = inner;
     a.chunks = qpack_chunks(inner);
     a.cold = cold;
+    const QuantCut cut = quant_cut_choice(c->rows, cols, inner, c->n_cus, max_pieces);
+    a.tile = cut.tile;
+    a.pieces = cut.pieces;
     launch_quant_linear(a, c->n_cus, st);
+    return cut.pieces;
 }
 // A single row takes the single query's attention, whose chunks the quantisation behind it merges in one workgroup, as long as
 // they are no more than this many floats; else rotation, the tree's attention and quantisation.  Layers of one row, tree's -> merged, us:
 // hidden 4096, no context 62.8 -> 59.8, 1024 rows 68.2 -> 61.6, 2048 70.0 -> 66.5, 3000 71.8 -> 70.3, 4200 77.0 -> 85.3; hidden 5120, 1024
 // rows 89.1 -> 85.1, 2048 91.7 -> 90.6, 3000 94.7 -> 98.0.
 constexpr int MERGED_FLOATS = 96 * 1024;
-// One layer; delta: the layer before has left its last product in c->part, still to be added to x, as this one does.  cold: see
-// QuantLinearArgs.
-void enqueue_layer_quantized(cats_ctx* c, const cats_quantized_layer* w, float* x, bool delta, bool cold, const cats_kv_layer* kv,
-                             int ctx_len, hipStream_t st) {
+// One layer; delta: the layer before has left its last product in c->part in that many pieces, still to be added to x, as this one
+// does (returned).  cold: see QuantLinearArgs.
+int enqueue_layer_quantized(cats_ctx* c, const cats_quantized_layer* w, float* x, int delta, bool cold, const cats_kv_layer* kv,
+                            int ctx_len, hipStream_t st) {
     const int H = c->d.hidden, F = c->d.ffn;
     enqueue_norm_quantized(c, x, delta, w->g_attn, st);
-    enqueue_linear_quantized(c, c->xn, H, w->w_qkv, w->s_qkv, 3 * H, cold, st);
-    const GemmPlan whole{1, GEMM_KC, 1, 1, 1};   // one complete piece
+    enqueue_linear_quantized(c, c->xn, H, w->w_qkv, w->s_qkv, 3 * H, 1, cold, st);
+    const GemmPlan whole = whole_pieces_plan(3 * H, 1);
     const NormScale as_is{c->ss_zero, (H + SS_COLS - 1) / SS_COLS, H, 1.f};   // norm factor 1 / sqrt(0 + 1)
     // The attention output is rounded to bf16 in front of 8 bits: its last bit is 2^-8 of a value, the step of the row 2^-7 of the
     // largest one.
@@ -575,12 +587,14 @@ void enqueue_layer_quantized(cats_ctx* c, const cats_quantized_layer* w, float* 
         a.src_type = CATS_BF16;
         launch_quant_rows(a, ROWS_PLAIN, st);
     }
-    enqueue_linear_quantized(c, c->xn, H, w->w_o, w->s_o, H, cold, st);
-    enqueue_norm_quantized(c, x, true, w->g_ffn, st);
-    enqueue_linear_quantized(c, c->xn, H, w->w_gate_up, w->s_gate_up, 2 * F, cold, st);
+    // (c->part holds 3 H columns at least)
+    const int pieces = enqueue_linear_quantized(c, c->xn, H, w->w_o, w->s_o, H, QUANT_MAX_PIECES, cold, st);
+    enqueue_norm_quantized(c, x, pieces, w->g_ffn, st);
+    enqueue_linear_quantized(c, c->xn, H, w->w_gate_up, w->s_gate_up, 2 * F, 1, cold, st);
     launch_quant_rows(quant_rows(c, c->part, 2 * static_cast<int64_t>(F), F, c->hact), ROWS_SWIGLU, st);
-    enqueue_linear_quantized(c, c->hact, F, w->w_down, w->s_down, H, cold, st);
+    return enqueue_linear_quantized(c, c->hact, F, w->w_down, w->s_down, H, QUANT_MAX_PIECES, cold, st);
 }
+static_assert(QUANT_MAX_PIECES <= 3, "c->part holds as many rows of hidden columns");
 
 RopeTableArgs rope_table_args(const cats_ctx* c, int ctx_len) {
     RopeTableArgs r;
@@ -931,15 +945,16 @@ int cats_verify_layers_quantized(cats_ctx* ctx, const cats_quantized_layer* laye
     // weights that the call reads: 4 H^2 + 3 H F bytes a layer, against a cache of 256 MB
     const int64_t H = ctx->d.hidden, F = ctx->d.ffn;
     const bool cold = (4 * H * H + 3 * H * F) * (layer_end - layer_begin) > int64_t{256} << 20;
+    int pieces = 0;
     for (int l = layer_begin; l < layer_end; ++l)
-        enqueue_layer_quantized(ctx, &layers[l], hidden, l > layer_begin, cold, &kv[l], ctx_len, st);
+        pieces = enqueue_layer_quantized(ctx, &layers[l], hidden, pieces, cold, &kv[l], ctx_len, st);
     ResidualNormArgs rn;   // the last layer's product
     rn.x = hidden;
     rn.x_in = nullptr;
     rn.embed = nullptr;
     rn.token = nullptr;
     rn.part = ctx->part;
-    rn.plan = GemmPlan{1, GEMM_KC, 1, 1, 1};
+    rn.plan = whole_pieces_plan(ctx->d.hidden, pieces);
     rn.gain = nullptr;
     rn.xn = ctx->xn;
     rn.xn_lo = ctx->xn_lo;

@@ -20,6 +20,7 @@ enum { ROWS_PLAIN = 0, ROWS_NORM = 1, ROWS_SWIGLU = 2, ROWS_MERGED = 3 };
 struct QuantRowsArgs {
     const void* src;       // float32 or bf16 (ROWS_NORM: float32; ROWS_MERGED: DecodeAttnArgs.po)
     const void* delta;     // ROWS_NORM, optional
+    int delta_pieces;      // more than one: float32 [delta_pieces][rows][delta_ld], to be added up first (QuantLinearArgs.pieces)
     const bf16_t* gain;    // ROWS_NORM: [cols]
     float* x_out;          // ROWS_NORM with delta: the updated rows (may be src)
     int8_t* q;
@@ -50,8 +51,12 @@ struct QuantLinearArgs {
     int rows, cols, inner;
     int chunks;            // packed chunks of 64 along inner, a multiple of four
     int y_type;
+    int pieces = 1;        // of the inner length, the sums of each times the scales in y + piece * rows * y_ld; float32, at most
+                           // QUANT_MAX_PIECES, and only with a tile of cats_quant_linear_split (quant_choice)
+    int tile = -1;         // one of QUANT_TILES, or -1: the best for one piece
     bool cold = false;     // the caller reads more weights than the caches hold before it reads these again
 };
+constexpr int QUANT_MAX_PIECES = 3;
 void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st);
 void launch_quant_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st);        // tiles of 256 x 256
 void launch_quant_tiles_half(const QuantLinearArgs& a, int n_cus, hipStream_t st);   // of 128 rows x 256 columns

@@ -19,17 +19,43 @@ constexpr QuantTile QUANT_TILES[] = {{16, 16, 32},   {16, 32, 50},   {16, 48, 70
                                      {64, 112, 176}, {64, 128, 192}, {96, 96, 192},  {128, 64, 192}, {128, 96, 250}, {96, 128, 288},
                                      {128, 112, 330}, {128, 128, 350}, {128, 256, 500}, {256, 256, 700}};
 constexpr int N_QUANT_TILES = sizeof(QUANT_TILES) / sizeof(QUANT_TILES[0]);
-inline int quant_tile_choice(int rows, int cols, int n_cus) {
+constexpr int N_QUANT_SPLIT_TILES = N_QUANT_TILES - 2;   // those whose kernel can take a piece of the inner length
+inline int quant_tile_choice(int rows, int cols, int n_cus, int pieces = 1, int64_t* cost_out = nullptr) {
     int best = 0;
     int64_t least = INT64_MAX;
-    for (int i = 0; i < N_QUANT_TILES; ++i) {
+    for (int i = 0; i < (pieces > 1 ? N_QUANT_SPLIT_TILES : N_QUANT_TILES); ++i) {
         const QuantTile& c = QUANT_TILES[i];
         if (rows <= 16 && c.bm > 16) break;
-        const int64_t tiles = ((int64_t{rows} + c.bm - 1) / c.bm) * ((int64_t{cols} + c.bn - 1) / c.bn);
+        const int64_t tiles = ((int64_t{rows} + c.bm - 1) / c.bm) * ((int64_t{cols} + c.bn - 1) / c.bn) * pieces;
         const int64_t cost = (tiles + n_cus - 1) / n_cus * c.cost;
         if (cost <= least) {   // of equals the larger tile: fewer bytes
             least = cost;
             best = i;
+        }
+    }
+    if (cost_out) *cost_out = least;
+    return best;
+}
+
+// Pieces of the inner length, each a product of its own, that the consumer adds up: where few columns make small tiles, larger
+// ones of a piece each read less (63 x 4096 x 11008 from memory 16.0 us in tiles of 32 x 32, 13.7 in two pieces of 64 x 32; 63 x 5120
+// x 13824 24.7 and in three of 64 x 64 17.2).  Every piece more is rows of float32 written and read and counts PIECE_COST at inner =
+// 4096.  Layers in 8 bits, us, one piece | cost 8 | 16 | 24: 7B-shaped, 63 nodes 93.7 | 92.6 | 92.6 | 92.8, 128 nodes 121.3 | 121.3 |
+// 119.4 | 119.4; 13B-shaped 123.7 | 116.6 | 116.7 | 116.6 and 166.6 | 161.0 | 161.0 | 159.2.
+struct QuantCut {
+    int tile, pieces;
+};
+constexpr int PIECE_COST = 24;
+inline QuantCut quant_cut_choice(int rows, int cols, int inner, int n_cus, int max_pieces) {
+    QuantCut best{0, 1};
+    int64_t least = INT64_MAX;
+    for (int p = 1; p <= (rows > 16 ? max_pieces : 1); ++p) {
+        int64_t cost;
+        const int tile = quant_tile_choice(rows, cols, n_cus, p, &cost);
+        cost = cost * inner / p + int64_t{PIECE_COST} * 4096 * (p - 1);
+        if (cost < least) {
+            least = cost;
+            best = {tile, p};
         }
     }
     return best;

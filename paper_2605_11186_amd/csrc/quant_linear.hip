@@ -42,10 +42,17 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
     __shared__ __align__(16) float s_sx[16 * MB], s_sw[16 * NB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int mt, nt;
-    quant_tile_of(blockIdx.x, m_tiles, n_tiles, mt, nt);
+    quant_tile_of(blockIdx.x, m_tiles, n_tiles * a.pieces, mt, nt);
     const int n_rb = (a.cols + QPACK_ROWS - 1) / QPACK_ROWS;
     const int k_last = (a.inner - 1) / 16 * 16;
-    const int steps = (a.inner + 127) >> 7;   // (the packed weights may have one step of zeros more)
+    int step0 = 0, steps = (a.inner + 127) >> 7;   // (the packed weights may have one step of zeros more)
+    if (a.pieces > 1) {
+        const int piece = nt / n_tiles, all = steps;
+        nt -= piece * n_tiles;
+        step0 = all * piece / a.pieces;
+        steps = all * (piece + 1) / a.pieces - step0;
+        a.y = static_cast<float*>(a.y) + static_cast<int64_t>(piece) * a.rows * a.y_ld;
+    }
     const int mine = (steps - wave + KW - 1) / KW;
 
     // the scales, for when the sums are ready
@@ -63,7 +70,7 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
     for (int j = 0; j < NB; ++j) wp[j] = a.w + static_cast<int64_t>(min(nt * NB + j, n_rb - 1)) * a.chunks * QPACK_FRAG;
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(&s_lds[0])) + wave * OWN;
     auto fetch_w = [&](int i, int slot) {   // for the i-th of this wave's steps
-        const int s = wave + i * KW;
+        const int s = step0 + wave + i * KW;
         const uint32_t to = lds0 + slot * NB * 2048;
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
@@ -72,7 +79,7 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
         }
     };
     auto fetch_x = [&](int i, int slot) {
-        const int k = min((wave + i * KW) * 128 + piece, k_last);
+        const int k = min((step0 + wave + i * KW) * 128 + piece, k_last);
         const uint32_t to = lds0 + (NW * NB + slot * MB) * 2048;
 #pragma unroll
         for (int p = 0; p < 2 * MB; ++p) copy_to_lds(x0, xo[p] + k, to + p * 1024);
@@ -153,7 +160,7 @@ void launch_split(const QuantLinearArgs& a, int, hipStream_t st) {
     // weights that come past the caches, one step further ahead where the LDS holds it (63 x 27648 x 5120 30.0 -> 28.2 us)
     constexpr int ONCE_NW = NW == 1 && MB >= 4 && (MB + 2 * NB) * 2048 * KW < 156 * 1024 ? 2 : NW;
     hipLaunchKernelGGL((once ? cats_quant_linear_split<MB, NB, KW, NS, ONCE_NW, true> : cats_quant_linear_split<MB, NB, KW, NS, NW, false>),
-                       dim3(static_cast<unsigned>(m_tiles) * n_tiles), dim3(64 * KW), 0, st, a, m_tiles, n_tiles);
+                       dim3(static_cast<unsigned>(m_tiles) * n_tiles * a.pieces), dim3(64 * KW), 0, st, a, m_tiles, n_tiles);
 }
 
 // One wave moves one kilobyte: rows of 64 values in, an operand of the matrix instruction out.  vec: rows start at multiples of
@@ -216,7 +223,7 @@ void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
         launch_split<8, 7, 4, 1, 1>, launch_split<8, 8, 4, 1, 1>,
         launch_quant_tiles_half, launch_quant_tiles};
     static_assert(sizeof(LAUNCH) / sizeof(LAUNCH[0]) == N_QUANT_TILES, "one kernel for each tile");
-    LAUNCH[quant_tile_choice(a.rows, a.cols, n_cus)](a, n_cus, st);
+    LAUNCH[a.tile < 0 ? quant_tile_choice(a.rows, a.cols, n_cus) : a.tile](a, n_cus, st);
 }
 
 extern "C" {

@@ -14,6 +14,9 @@
 namespace {
 
 typedef double none_t;   // the type of a delta that is not there
+struct pieces_t {        // a delta of several pieces
+    float v;
+};
 
 constexpr float SCALE_MIN = 0x1p-126f;   // smallest normal number: 1 / scale stays finite
 
@@ -193,17 +196,30 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
         Raw<bf16_t, VEC> rg[NC];
         float ss = 0.f;
         if constexpr (HAS_DELTA) {
-            Raw<D, VEC> r1[NC];
-            const D* delta = static_cast<const D*>(a.delta) + t * a.delta_ld;
+            // PIECES loads of each value at once; those of pieces that are not there are the last one's again, and do not count
+            constexpr bool PIECED = std::is_same<D, pieces_t>::value;
+            constexpr int PIECES = PIECED ? QUANT_MAX_PIECES : 1;
+            using E = typename std::conditional<PIECED, float, D>::type;
+            Raw<E, VEC> r1[PIECES][NC];
+            const E* delta = static_cast<const E*>(a.delta) + t * a.delta_ld;
             float* out = a.x_out + t * a.x_out_ld;
 #pragma unroll
-            for (int j = 0; j < NC; ++j) r1[j] = load8<D, TPR, VEC>(delta, tid, j, cols);
+            for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+                for (int j = 0; j < NC; ++j)
+                    r1[p][j] = load8<E, TPR, VEC>(delta + (PIECED ? min(p, a.delta_pieces - 1) * (a.rows * a.delta_ld) : 0), tid, j, cols);
 #pragma unroll
             for (int j = 0; j < NC; ++j) rg[j] = load8<bf16_t, TPR, VEC>(a.gain, tid, j, cols);
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[j][e] = in[j][VEC ? 0 : e] ? r0[j].get(e) + r1[j].get(e) : 0.f;
+                for (int e = 0; e < 8; ++e) {
+                    float sum = r1[0][j].get(e);
+#pragma unroll
+                    for (int p = 1; p < PIECES; ++p)
+                        if (p < a.delta_pieces) sum += r1[p][j].get(e);
+                    v[j][e] = in[j][VEC ? 0 : e] ? r0[j].get(e) + sum : 0.f;
+                }
                 if constexpr (VEC) {
                     if (in[j][0]) {
                         f32x4* p = reinterpret_cast<f32x4*>(out + place<TPR, VEC>(tid, j, 0));
@@ -370,6 +386,7 @@ void launch_quant_rows(const QuantRowsArgs& a, int kind, hipStream_t st) {
     if (kind == ROWS_SWIGLU)
         return f32 ? by_alignment<ROWS_SWIGLU, float, none_t>(a, st) : by_alignment<ROWS_SWIGLU, bf16_t, none_t>(a, st);
     if (!a.delta) return by_alignment<ROWS_NORM, float, none_t>(a, st);
+    if (a.delta_pieces > 1) return by_alignment<ROWS_NORM, float, pieces_t>(a, st);
     return a.delta_type == CATS_F32 ? by_alignment<ROWS_NORM, float, float>(a, st)
                                     : by_alignment<ROWS_NORM, float, bf16_t>(a, st);
 }

@@ -195,6 +195,49 @@ def test_a_single_node_as_the_root_of_two(hidden, ctx_len):
         cats.cats_destroy(ctx)
 
 
+# hidden, feed-forward columns and nodes at which the output and down products come in 2 and 3 pieces (test_quant_choice checks that)
+PIECES = [(4096, 11008, 63, (1, 2)), (5120, 13824, 63, (2, 3)), (4096, 11008, 128, (2, 2)), (2048, 8192, 40, (1, 2)),
+          (7168, 1024, 90, (3, 1))]
+
+
+@pytest.mark.parametrize("zero", ["wo", "w_down"])
+@pytest.mark.parametrize("hidden,ffn,nodes", [p[:3] for p in PIECES])
+def test_products_in_pieces(hidden, ffn, nodes, zero):
+    """A layer over a tree and over its first 16 nodes, for which no product is cut.  With an output product of zeros the down product
+    has the same bytes to multiply in both, in all rows; with a down product of zeros the output product has for the root, which
+    behind no context sees itself alone.  So the rows differ by float32 roundings: for each of at most three pieces p three in the
+    scales and two in the sum, three for the whole product y, one each where x comes on top.  y and p are sums of random signs, |p| <= 2
+    max|y| = 2 Y for certain: 2^-24 (5 * 3 * 2 Y + 3 Y + 2 max|h|), Y <= max|h| + max|x| <= 2 max|h| or it is smaller still: 68 * 2^-24."""
+    heads = hidden // 128
+    gen = torch.Generator(device="cuda").manual_seed(29)
+
+    def random(*shape, by=0.02):
+        return torch.empty(*shape, device="cuda").normal_(0, by, generator=gen).to(torch.bfloat16)
+
+    one = torch.ones(hidden, dtype=torch.bfloat16, device="cuda")
+    weights = dict(wq=random(hidden, hidden), wk=random(hidden, hidden), wv=random(hidden, hidden), wo=random(hidden, hidden),
+                   w_gate=random(ffn, hidden), w_up=random(ffn, hidden), w_down=random(hidden, ffn), g_attn=one, g_ffn=one)
+    weights[zero].zero_()
+    layer, ctx_len = cats.quantize_layer(weights), 150 if zero == "wo" else 0
+    ctx = cats.cats_create(cats.ModelDesc(1, hidden, heads, 128, ffn, 1000, 320, 128, 1e-6, 1e4, 0))
+    try:
+        k, v = random(heads, 320, 128, by=1), random(heads, 128, 320, by=1)
+        x = torch.empty(nodes, hidden, device="cuda").normal_(generator=gen)
+        parent, depth = tree_of(nodes, 7)
+        rows = []
+        for n in (nodes, 16):
+            h = x[:n].clone()
+            cats.cats_set_tree(ctx, np.zeros(n, np.int32), parent[:n], depth[:n])
+            cats.cats_verify_layers_quantized(ctx, cats.quantized_layer_array([layer]), 0, 1, h, cats.kv_array([k], [v]), ctx_len)
+            torch.cuda.synchronize()
+            rows.append(h[:16 if zero == "wo" else 1])
+        assert torch.isfinite(rows[0]).all() and (rows[0] - x[:len(rows[0])]).abs().max() > 1
+        assert (rows[0] - rows[1]).abs().max() <= 68 * 2.0 ** -24 * rows[1].abs().max()
+    finally:
+        torch.cuda.synchronize()
+        cats.cats_destroy(ctx)
+
+
 @pytest.mark.parametrize("nodes", [1, 20, 63, 128])
 def test_a_call_whose_weights_pass_the_caches(nodes):
     """Two layers of 202 MB of weights in one call (past the caches) and one after the other (through them): the same bits."""

@@ -6,6 +6,7 @@ import pytest
 
 import host_shim
 from test_gpu_quant import ONCE_SIZES, TILE_SIZES
+from test_gpu_quant_layers import PIECES
 
 SHIM = """
 #include "quant_choice.hpp"
@@ -13,6 +14,8 @@ extern "C" {
 int n_tiles() { return N_QUANT_TILES; }
 int tile(int i, int what) { return what == 0 ? QUANT_TILES[i].bm : what == 1 ? QUANT_TILES[i].bn : QUANT_TILES[i].cost; }
 int choice(int rows, int cols, int n_cus) { return quant_tile_choice(rows, cols, n_cus); }
+int pieces(int rows, int cols, int inner, int n_cus, int most) { return quant_cut_choice(rows, cols, inner, n_cus, most).pieces; }
+int cut_tile(int rows, int cols, int inner, int n_cus, int most) { return quant_cut_choice(rows, cols, inner, n_cus, most).tile; }
 }
 """
 
@@ -65,3 +68,16 @@ def test_the_choice_costs_least(rule):
                 costs = [-(-(-(-rows // rule.tile(i, 0)) * -(-cols // rule.tile(i, 1))) // n_cus) * rule.tile(i, 2)
                          for i in range(rule.n_tiles()) if rows > 16 or rule.tile(i, 0) == 16]
                 assert costs[rule.choice(rows, cols, n_cus)] == min(costs)
+
+
+def test_pieces_of_the_inner_length(rule):
+    """One piece: the tile of the whole product.  More: a tile of the kernel that can take pieces, and not for up to 16 rows."""
+    for hidden, ffn, nodes, want in PIECES:
+        assert (rule.pieces(nodes, hidden, hidden, 256, 3), rule.pieces(nodes, hidden, ffn, 256, 3)) == want, (hidden, nodes)
+    for rows in (1, 16, 17, 63, 128):
+        for cols in (64, 512, 4096, 8192):
+            for inner in (16, 64, 4096, 65536):
+                assert rule.cut_tile(rows, cols, inner, 256, 1) == rule.choice(rows, cols, 256)
+                p = rule.pieces(rows, cols, inner, 256, 3)
+                assert p in (1, 2, 3) and (rows > 16 or p == 1) and (p == 1 or inner >= 128 * p)
+                assert p == 1 or rule.cut_tile(rows, cols, inner, 256, 3) < rule.n_tiles() - 2
