@@ -214,7 +214,8 @@ def test_products_in_pieces(hidden, ffn, nodes, zero):
     def random(*shape, by=0.02):
         return torch.empty(*shape, device="cuda").normal_(0, by, generator=gen).to(torch.bfloat16)
 
-    one = torch.ones(hidden, dtype=torch.bfloat16, device="cuda")
+    # gains at an odd multiple of two bytes make the norms read value by value
+    one = torch.ones(hidden + 1, dtype=torch.bfloat16, device="cuda")[zero == "w_down":][:hidden]
     weights = dict(wq=random(hidden, hidden), wk=random(hidden, hidden), wv=random(hidden, hidden), wo=random(hidden, hidden),
                    w_gate=random(ffn, hidden), w_up=random(ffn, hidden), w_down=random(hidden, ffn), g_attn=one, g_ffn=one)
     weights[zero].zero_()
