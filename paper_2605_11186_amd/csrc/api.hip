@@ -535,7 +535,7 @@ int enqueue_linear_quantized(cats_ctx* c, const void* q, int inner, const int8_t
     a.chunks = qpack_chunks(inner);
     a.cold = cold;
     const QuantCut cut = quant_cut_choice(c->rows, cols, inner, c->n_cus, max_pieces);
-    a.tile = cut.tile;
+    if (cut.pieces > 1) a.tile = cut.tile;
     a.pieces = cut.pieces;
     launch_quant_linear(a, c->n_cus, st);
     return cut.pieces;

@@ -58,8 +58,10 @@ struct QuantLinearArgs {
 };
 constexpr int QUANT_MAX_PIECES = 3;
 void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st);
-void launch_quant_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st);        // tiles of 256 x 256
-void launch_quant_tiles_half(const QuantLinearArgs& a, int n_cus, hipStream_t st);   // of 128 rows x 256 columns
+void launch_quant_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st);               // tiles of 256 x 256
+void launch_quant_tiles_narrow(const QuantLinearArgs& a, int n_cus, hipStream_t st);        // of 256 rows x 192 columns
+void launch_quant_tiles_half(const QuantLinearArgs& a, int n_cus, hipStream_t st);          // of 128 rows x 256 columns
+void launch_quant_tiles_half_narrow(const QuantLinearArgs& a, int n_cus, hipStream_t st);   // of 128 rows x 192 columns
 
 // 64 lanes copy 16 bytes each from base + their own offset to 1024 consecutive bytes of LDS (at byte `lds`), with no
 // register between.  Counted in vmcnt like a load; the compiler does not see it and waits for nothing on its account.

@@ -17,9 +17,10 @@ struct QuantTile {
 constexpr QuantTile QUANT_TILES[] = {{16, 16, 32},   {16, 32, 50},   {16, 48, 70},   {32, 16, 48},   {32, 32, 64},   {32, 48, 80},   {32, 64, 96},
                                      {32, 96, 128},  {32, 112, 144}, {32, 128, 160}, {64, 32, 96},   {64, 48, 112},  {64, 64, 128},  {64, 96, 160},
                                      {64, 112, 176}, {64, 128, 192}, {96, 96, 192},  {128, 64, 192}, {128, 96, 250}, {96, 128, 288},
-                                     {128, 112, 330}, {128, 128, 350}, {128, 256, 500}, {256, 256, 700}};
+                                     {128, 112, 330}, {128, 128, 350}, {128, 192, 420}, {128, 256, 500},
+                                     {256, 192, 600}, {256, 256, 700}};
 constexpr int N_QUANT_TILES = sizeof(QUANT_TILES) / sizeof(QUANT_TILES[0]);
-constexpr int N_QUANT_SPLIT_TILES = N_QUANT_TILES - 2;   // those whose kernel can take a piece of the inner length
+constexpr int N_QUANT_SPLIT_TILES = N_QUANT_TILES - 4;   // those whose kernel can take a piece of the inner length
 inline int quant_tile_choice(int rows, int cols, int n_cus, int pieces = 1, int64_t* cost_out = nullptr) {
     int best = 0;
     int64_t least = INT64_MAX;
@@ -34,6 +35,37 @@ inline int quant_tile_choice(int rows, int cols, int n_cus, int pieces = 1, int6
         }
     }
     if (cost_out) *cost_out = least;
+    return best;
+}
+
+// Many rows: tiles that fill a round of compute units and a few more leave the chip idle for most of the next one.  Then the first
+// columns, whole rounds of one of the four largest tiles, are one launch and the others another, in the tiles that suit them best.
+// 700 x 22016 x 4096 90 us as 258 tiles of 256 x 256, 66.5 as 255 of them and 256 columns in tiles of 32 x 32; 1500 x 12288 x 4096 88 and
+// 73.  The tiles of 192 columns fill the chip where those of 256 do not: 256 x 22016 x 4096 43.6 -> 37.0, 300 x 15360 x 5120 43.5 -> 35.5.
+struct QuantPlan {
+    int tile, cols;     // of the first launch; cols: all of them, or the first ones, a multiple of 64
+    int rest_tile;      // of the second, if there is one
+};
+constexpr int LAUNCH_COST = 40;   // of the second launch, at inner = 4096
+inline QuantPlan quant_plan(int rows, int cols, int inner, int n_cus) {
+    int64_t least;
+    QuantPlan best{quant_tile_choice(rows, cols, n_cus, 1, &least), cols, 0};
+    if (rows <= 128) return best;
+    least *= inner;
+    for (int i = N_QUANT_SPLIT_TILES; i < N_QUANT_TILES; ++i) {
+        const QuantTile& c = QUANT_TILES[i];
+        const int64_t m_tiles = (int64_t{rows} + c.bm - 1) / c.bm, n_tiles = (int64_t{cols} + c.bn - 1) / c.bn;
+        const int64_t rounds = m_tiles * n_tiles / n_cus, n_main = rounds * n_cus / m_tiles;
+        if (n_main < 1 || n_main == n_tiles) continue;
+        const int main_cols = static_cast<int>(n_main) * c.bn;
+        int64_t rest;
+        const int rest_tile = quant_tile_choice(rows, cols - main_cols, n_cus, 1, &rest);
+        const int64_t cost = ((m_tiles * n_main + n_cus - 1) / n_cus * c.cost + rest) * inner + int64_t{LAUNCH_COST} * 4096;
+        if (cost < least) {
+            least = cost;
+            best = {i, main_cols, rest_tile};
+        }
+    }
     return best;
 }
 

@@ -221,9 +221,19 @@ void launch_quant_linear(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
         launch_split<4, 4, 4, 1, 1>, launch_split<4, 6, 4, 1, 1>, launch_split<4, 7, 4, 1, 1>, launch_split<4, 8, 4, 1, 1>,
         launch_split<6, 6, 4, 1, 1>, launch_split<8, 4, 4, 1, 1>, launch_split<8, 6, 4, 1, 1>, launch_split<6, 8, 4, 1, 1>,
         launch_split<8, 7, 4, 1, 1>, launch_split<8, 8, 4, 1, 1>,
-        launch_quant_tiles_half, launch_quant_tiles};
+        launch_quant_tiles_half_narrow, launch_quant_tiles_half, launch_quant_tiles_narrow, launch_quant_tiles};
     static_assert(sizeof(LAUNCH) / sizeof(LAUNCH[0]) == N_QUANT_TILES, "one kernel for each tile");
-    LAUNCH[a.tile < 0 ? quant_tile_choice(a.rows, a.cols, n_cus) : a.tile](a, n_cus, st);
+    if (a.tile >= 0) return LAUNCH[a.tile](a, n_cus, st);
+    const QuantPlan plan = quant_plan(a.rows, a.cols, a.inner, n_cus);
+    QuantLinearArgs part = a;
+    part.cols = plan.cols;
+    LAUNCH[plan.tile](part, n_cus, st);
+    if (plan.cols == a.cols) return;
+    part.cols = a.cols - plan.cols;
+    part.w = a.w + static_cast<int64_t>(plan.cols / QPACK_ROWS) * a.chunks * QPACK_FRAG;
+    part.w_scale = a.w_scale + plan.cols;
+    part.y = static_cast<char*>(a.y) + static_cast<int64_t>(plan.cols) * (a.y_type == CATS_F32 ? 4 : 2);
+    LAUNCH[plan.rest_tile](part, n_cus, st);
 }
 
 extern "C" {

@@ -20,7 +20,7 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
     constexpr int WAVES = WM * WN, BM = 16 * WM * MB, BN = 16 * WN * NB;
     constexpr int COPIES = BM / 8 / WAVES;   // of a wave and step: 8 rows of 128 bytes each
     static_assert(4 % WS == 0, "places of W come round again after a pair of steps");
-    static_assert(MB % NB == 0 && 2 * MB % COPIES == 0, "requests dealt evenly");
+    static_assert(MB >= NB && 2 * MB % COPIES == 0, "requests dealt evenly");
     static_assert(COPIES * 8 * WAVES == BM, "rows dealt evenly");
     constexpr int ROW = 16 * NB * 2 + 16;   // bytes of a row of y on its way out: data and 16, so that rows start at different banks
     __shared__ __align__(1024) int8_t s_x[NS][BM * 128];
@@ -109,17 +109,21 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
 #pragma unroll
         for (int f = 0; f < 2 * MB; ++f) {
             const int i = f % MB, h = f / MB;
-            if (i % (MB / NB) == 0) w[(2 * u + h + WS - 1) % WS][i / (MB / NB)] = load_w(2 * s + h + WS - 1, i / (MB / NB));
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                if (i == j * MB / NB) w[(2 * u + h + WS - 1) % WS][j] = load_w(2 * s + h + WS - 1, j);
             if (f % (2 * MB / COPIES) == 1) copy_piece(s + NS - 1, slot == 0 ? NS - 1 : slot - 1, f / (2 * MB / COPIES));
             const i32x4 xf = x[f % AHEAD];
             x[f % AHEAD] = f + AHEAD < 2 * MB ? read_x(slot, f + AHEAD) : read_x(slot1, f + AHEAD - 2 * MB);
 #pragma unroll
             for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[(2 * u + h) % WS][j], xf, acc[i][j], 0, 0, 0);
         }
-        // the order of the step: a fragment of X for each that is multiplied, a request for W at each second
+        // the order of the step: a fragment of X for each that is multiplied, the requests for W between them
 #pragma unroll
         for (int f = 0; f < 2 * MB; ++f) {
-            if (f % (MB / NB) == 0) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                if (f % MB == j * MB / NB) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
@@ -174,8 +178,9 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
                 __builtin_amdgcn_wave_barrier();
                 constexpr int LANES = 2 * NB;   // of a row
 #pragma unroll
-                for (int k = 0; k < 16 * LANES / 64; ++k) {
-                    const int row = k * (64 / LANES) + lane / LANES, at16 = lane % LANES;
+                for (int k = 0; k < (16 * LANES + 63) / 64; ++k) {
+                    const int row = (k * 64 + lane) / LANES, at16 = (k * 64 + lane) % LANES;
+                    if (16 * LANES % 64 != 0 && row >= 16) break;
                     const u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * ROW + at16 * 16);
                     if (t + row < a.rows) *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.y) + (t + row) * a.y_ld + n0 + at16 * 8) = v;
                 }
@@ -200,4 +205,6 @@ void launch_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
 }  // namespace
 
 void launch_quant_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st) { launch_tiles<2, 4, 8, 4, 4, 4>(a, n_cus, st); }
+void launch_quant_tiles_narrow(const QuantLinearArgs& a, int n_cus, hipStream_t st) { launch_tiles<2, 4, 8, 3, 4, 4>(a, n_cus, st); }
 void launch_quant_tiles_half(const QuantLinearArgs& a, int n_cus, hipStream_t st) { launch_tiles<2, 4, 4, 4, 4, 4>(a, n_cus, st); }
+void launch_quant_tiles_half_narrow(const QuantLinearArgs& a, int n_cus, hipStream_t st) { launch_tiles<2, 4, 4, 3, 4, 4>(a, n_cus, st); }

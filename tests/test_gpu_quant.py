@@ -260,7 +260,8 @@ TILE_SIZES = {(16, 16): (13, 1003), (16, 32): (9, 4107), (16, 48): (9, 12001), (
               (32, 48): (29, 12001), (32, 64): (31, 15307), (32, 96): (29, 21001), (32, 112): (27, 27001), (32, 128): (31, 32001),
               (64, 32): (62, 8001), (64, 48): (57, 10007), (64, 64): (254, 4077), (64, 96): (61, 21001), (64, 112): (61, 27001),
               (64, 128): (63, 32001), (96, 96): (95, 21001), (128, 64): (509, 4077), (128, 96): (125, 21001), (96, 128): (763, 4077),
-              (128, 112): (125, 27001), (128, 128): (1021, 4077), (128, 256): (2001, 4077), (256, 256): (4001, 4077)}
+              (128, 112): (125, 27001), (128, 128): (1021, 4077), (128, 192): (500, 12201), (128, 256): (2001, 4077),
+              (256, 192): (1001, 12201), (256, 256): (4001, 4077)}
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
@@ -285,10 +286,24 @@ def test_linear_weights_past_the_caches(tile):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("rows,cols,inner", [(4001, 4177, 333), (3800, 8200, 1290), (300, 43501, 333), (513, 33000, 600)])
+@pytest.mark.parametrize("rows,cols,inner", [(4001, 4177, 333), (3800, 8200, 1290), (300, 43501, 333), (513, 33000, 600), (999, 24504, 333),
+                                             (500, 12200, 333)])
 def test_linear_several_tiles_a_workgroup(rows, cols, inner, dtype):
-    """More of the largest tiles than compute units: a workgroup's next tile is under way while it stores one."""
+    """More of the largest tiles than compute units: a workgroup's next tile is under way while it stores one.  (The last size: whole
+    lines of y from tiles of 192 columns.)"""
     run_linear(rows, cols, inner, dtype)
+
+
+# sizes whose last columns are a launch of their own (tests/test_quant_choice.py)
+CUT_SIZES = [(700, 22001, 2000), (700, 22008, 2000), (4001, 12501, 333), (1500, 10800, 1000)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols,inner", CUT_SIZES)
+def test_linear_in_two_launches(rows, cols, inner, dtype):
+    run_linear(rows, cols, inner, dtype)
+    if rows == 700:
+        run_linear(rows, cols, inner, dtype, x_ld=2016, y_ld=22017)
 
 
 @pytest.mark.parametrize("rows", [1, 40, 130, 520])
