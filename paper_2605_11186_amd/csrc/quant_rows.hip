@@ -36,6 +36,12 @@ __device__ __forceinline__ uint32_t wave_max64(uint32_t v) {
     return max(v, dpp_moved_u<0xB1>(v));
 }
 
+// 1 / sqrt(x) for x > 0, to 1 ulp: the hardware's, which takes no numbers below the normal ones.
+__device__ __forceinline__ float inverse_sqrt(float x) {
+    const bool small = x < 0x1p-96f;
+    return __builtin_amdgcn_rsqf(small ? x * 0x1p96f : x) * (small ? 0x1p48f : 1.f);
+}
+
 // Eight values as they lie in memory: whole pieces of 16 bytes (VEC) or one by one.
 template <class T, bool VEC>
 struct Raw;
@@ -155,6 +161,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
     constexpr bool HAS_DELTA = !std::is_same<D, none_t>::value;
     const int tid = threadIdx.x % TPR;
     const int t = blockIdx.x * ROWS_WG + threadIdx.x / TPR;
+    // all arguments at once: loaded where they are used, they are several scalar round trips one behind the other
+    asm volatile("" ::"s"(a.src), "s"(a.src_ld), "s"(a.q), "s"(a.q_ld), "s"(a.scale), "s"(a.rows), "s"(a.cols));
+    if constexpr (KIND == ROWS_NORM) asm volatile("" ::"s"(a.gain), "s"(a.eps));
+    if constexpr (HAS_DELTA) asm volatile("" ::"s"(a.delta), "s"(a.delta_ld), "s"(a.x_out), "s"(a.x_out_ld));
     if (t >= a.rows) return;   // whole waves, and no barrier where a workgroup has several rows
     const int cols = a.cols;
     const T* src = static_cast<const T*>(a.src) + t * a.src_ld;
@@ -254,11 +264,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
             for (int w = 0; w < WAVES; ++w) ss += s_sum[w];
         }
         // a sum of squares beyond float32 makes the row not a number, as an infinity in it does
-        const float r = ss < INFINITY ? 1.f / sqrtf(ss / static_cast<float>(cols) + a.eps) : NAN;
+        const float r = ss < INFINITY ? inverse_sqrt(ss * (1.f / static_cast<float>(cols)) + a.eps) : NAN;
+        // (values that are not there are zeros, and NaN only where r or the last gains make the row's last values so, too)
 #pragma unroll
         for (int j = 0; j < NC; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[j][e] = in[j][VEC ? 0 : e] ? v[j][e] * r * rg[j].get(e) : 0.f;
+            for (int e = 0; e < 8; ++e) v[j][e] = v[j][e] * r * rg[j].get(e);
     }
 
     // the largest |v|, as bits: ordered like the numbers, infinity above them and NaN above infinity
@@ -277,7 +288,6 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
     }
     const bool finite = top < 0x7F800000u;
     const float most = fmaxf(__uint_as_float(top), 127.f * SCALE_MIN);
-    if (tid == 0) a.scale[t] = finite ? most / 127.f : NAN;
     // y + 1.5 * 2^23: the sum's last bits are the whole number nearest to y in two's complement (ties to even)
     constexpr float WHOLE = 12582912.f;
     // ROWS_PLAIN, ROWS_MERGED: y = 127 v / most as a correctly rounded quotient (by one correction), so that ties, which are common among bf16
@@ -285,7 +295,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
     // worth the three instructions a value.
     const float p = __uint_as_float(max(0x7F000000u - (__float_as_uint(most) & 0x7F800000u), 0x00800000u));
     constexpr bool TIES = KIND == ROWS_PLAIN || KIND == ROWS_MERGED;
-    const float den = TIES ? most * p : most, mul = TIES ? 127.f * p : 127.f / most, rden = 1.f / den;
+    const float den = most * p, rden = TIES ? 1.f / den : __builtin_amdgcn_rcpf(den), mul = 127.f * p * (TIES ? 1.f : rden);
     auto whole = [&](float v) {
         if constexpr (TIES) {
             const float z = v * mul, y = z * rden;
@@ -310,6 +320,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
                 if (in[j][e]) q[place<TPR, VEC>(tid, j, e)] = static_cast<int8_t>(b[e]);
         }
     }
+    if (tid == 0) a.scale[t] = finite ? most / 127.f : NAN;
 }
 
 template <int KIND, class T, class D, int TPR, int NC, bool VEC>
