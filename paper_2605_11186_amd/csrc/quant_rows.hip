@@ -74,17 +74,23 @@ template <int TPR, bool VEC>
 __device__ __forceinline__ int place(int tid, int j, int e) {
     return VEC ? (j * TPR + tid) * 8 + e : (j * 8 + e) * TPR + tid;
 }
-// Places behind the row read its last values instead (nothing counts of them): the loads need no branch.
+// A row as a buffer of its own: what lies behind it reads as zero and is not written (the buffer's range check), so that the
+// loads and stores need no branch and the values no select.  VEC only; else places behind the row read its last value, which counts
+// for nothing.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const void* row, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(row), 0, bytes, 0x00020000);
+}
 template <class T, int TPR, bool VEC>
 __device__ __forceinline__ Raw<T, VEC> load8(const T* row, int tid, int j, int cols) {
     Raw<T, VEC> r;
     if constexpr (VEC) {
-        const T* p = row + min(place<TPR, VEC>(tid, j, 0), cols - 8);
+        const __amdgpu_buffer_rsrc_t buf = row_buffer(row, cols * static_cast<int>(sizeof(T)));
+        const int at = place<TPR, VEC>(tid, j, 0) * static_cast<int>(sizeof(T));
         if constexpr (sizeof(T) == 4) {
-            r.v[0] = *reinterpret_cast<const f32x4*>(p);
-            r.v[1] = *reinterpret_cast<const f32x4*>(p + 4);
+            r.v[0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(buf, at, 0, 0));
+            r.v[1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(buf, at + 16, 0, 0));
         } else {
-            r.v = *reinterpret_cast<const u32x4*>(p);
+            r.v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buf, at, 0, 0));
         }
     } else {
 #pragma unroll
@@ -160,7 +166,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
     constexpr int WAVES = TPR / 64;
     constexpr bool HAS_DELTA = !std::is_same<D, none_t>::value;
     const int tid = threadIdx.x % TPR;
-    const int t = blockIdx.x * ROWS_WG + threadIdx.x / TPR;
+    const int t = __builtin_amdgcn_readfirstlane(blockIdx.x * ROWS_WG + threadIdx.x / TPR);   // (a wave's threads share a row)
     // all arguments at once: loaded where they are used, they are several scalar round trips one behind the other
     asm volatile("" ::"s"(a.src), "s"(a.src_ld), "s"(a.q), "s"(a.q_ld), "s"(a.scale), "s"(a.rows), "s"(a.cols));
     if constexpr (KIND == ROWS_NORM) asm volatile("" ::"s"(a.gain), "s"(a.eps));
@@ -182,7 +188,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
 #pragma unroll
         for (int j = 0; j < NC; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[j][e] = in[j][VEC ? 0 : e] ? r0[j].get(e) : 0.f;
+            for (int e = 0; e < 8; ++e) v[j][e] = VEC || in[j][e] ? r0[j].get(e) : 0.f;
     } else if constexpr (KIND == ROWS_MERGED) {
         merge_chunks<TPR, NC>(a, tid, v);
 #pragma unroll
@@ -200,7 +206,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
                 const float g = r0[j].get(e);
                 // (the hardware's reciprocal, 1 ulp: a division's ten instructions more made one row of 11008 take 4.4 us)
                 const float h = g * __builtin_amdgcn_rcpf(1.f + __expf(-g)) * r1[j].get(e);
-                v[j][e] = in[j][VEC ? 0 : e] ? h : 0.f;
+                v[j][e] = VEC || in[j][e] ? h : 0.f;
             }
     } else {
         Raw<bf16_t, VEC> rg[NC];
@@ -228,14 +234,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
 #pragma unroll
                     for (int p = 1; p < PIECES; ++p)
                         if (p < a.delta_pieces) sum += r1[p][j].get(e);
-                    v[j][e] = in[j][VEC ? 0 : e] ? r0[j].get(e) + sum : 0.f;
+                    v[j][e] = VEC || in[j][e] ? r0[j].get(e) + sum : 0.f;
                 }
                 if constexpr (VEC) {
-                    if (in[j][0]) {
-                        f32x4* p = reinterpret_cast<f32x4*>(out + place<TPR, VEC>(tid, j, 0));
-                        p[0] = f32x4{v[j][0], v[j][1], v[j][2], v[j][3]};
-                        p[1] = f32x4{v[j][4], v[j][5], v[j][6], v[j][7]};
-                    }
+                    const __amdgpu_buffer_rsrc_t buf = row_buffer(out, cols * 4);
+                    const int at = place<TPR, VEC>(tid, j, 0) * 4;
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[j][0], v[j][1], v[j][2], v[j][3]}), buf, at, 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[j][4], v[j][5], v[j][6], v[j][7]}), buf, at + 16, 0, 0);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
@@ -247,7 +252,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
             for (int j = 0; j < NC; ++j) {
                 rg[j] = load8<bf16_t, TPR, VEC>(a.gain, tid, j, cols);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[j][e] = in[j][VEC ? 0 : e] ? r0[j].get(e) : 0.f;
+                for (int e = 0; e < 8; ++e) v[j][e] = VEC || in[j][e] ? r0[j].get(e) : 0.f;
             }
         }
 #pragma unroll
@@ -311,9 +316,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
 #pragma unroll
         for (int e = 0; e < 8; ++e) b[e] = finite ? whole(v[j][e]) & 0xFFu : 0u;
         if constexpr (VEC) {
-            if (in[j][0])
-                *reinterpret_cast<uint2*>(q + place<TPR, VEC>(tid, j, 0)) =
-                    make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+            __builtin_amdgcn_raw_buffer_store_b64(u32x2{b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24},
+                                                  row_buffer(q, cols), place<TPR, VEC>(tid, j, 0), 0, 0);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
