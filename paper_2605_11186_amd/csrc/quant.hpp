@@ -1,6 +1,7 @@
 // Argument blocks and launchers of the operators in 8-bit integers (see cats.h for what they compute).
 #pragma once
 #include "common.hpp"
+#include "fast_div.hpp"
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
@@ -74,16 +75,34 @@ __device__ __forceinline__ void copy_to_lds(const int8_t* base, uint32_t offset,
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
 }
 
+// The tiles of a launch, n_tiles of them side by side for each piece, and what they are divided by.
+constexpr int QUANT_BAND = 4;
+struct QuantGrid {
+    int m_tiles, n_tiles, all;         // all: m_tiles * n_tiles * pieces
+    int band;                          // tiles of a band of QUANT_BAND row tiles
+    FastDiv by_band, by_last, by_n;    // by_last: the row tiles of the last band, if it has fewer
+};
+inline QuantGrid quant_grid(int rows, int cols, int pieces, int bm, int bn) {
+    QuantGrid g;
+    g.m_tiles = (rows + bm - 1) / bm;
+    g.n_tiles = (cols + bn - 1) / bn;
+    g.all = g.m_tiles * g.n_tiles * pieces;
+    g.band = QUANT_BAND * g.n_tiles * pieces;
+    g.by_band = make_fast_div(g.band);
+    g.by_last = make_fast_div(g.m_tiles % QUANT_BAND);
+    g.by_n = make_fast_div(g.n_tiles);
+    return g;
+}
 // Tile number `index` (of a launch's workgroups).  Workgroup b runs on XCD b % 8: an XCD takes a run of tiles, in bands of 4 row
 // tiles (a run of tiles of one band shares rows of X and of W in the XCD's L2).
-__device__ __forceinline__ void quant_tile_of(int index, int m_tiles, int n_tiles, int& mt, int& nt) {
-    constexpr int BAND = 4;
-    const int total = m_tiles * n_tiles, xcd = index & 7;
-    const int id = xcd * (total >> 3) + min(xcd, total & 7) + (index >> 3);
-    const int band = id / (BAND * n_tiles), in_band = id - band * BAND * n_tiles;
-    const int band_rows = min(BAND, m_tiles - band * BAND);
-    mt = __builtin_amdgcn_readfirstlane(band * BAND + in_band % band_rows);
-    nt = __builtin_amdgcn_readfirstlane(in_band / band_rows);
+__device__ __forceinline__ void quant_tile_of(const QuantGrid& g, int index, int& mt, int& nt) {
+    const int xcd = index & 7;
+    const int id = xcd * (g.all >> 3) + min(xcd, g.all & 7) + (index >> 3);
+    const int band = fast_div(id, g.by_band), in_band = id - band * g.band;
+    const int band_rows = min(QUANT_BAND, g.m_tiles - band * QUANT_BAND);
+    nt = band_rows == QUANT_BAND ? in_band / QUANT_BAND : static_cast<int>(fast_div(in_band, g.by_last));
+    mt = __builtin_amdgcn_readfirstlane(band * QUANT_BAND + in_band - nt * band_rows);
+    nt = __builtin_amdgcn_readfirstlane(nt);
 }
 
 // Four neighbouring columns of y from their sums; sums times the row's scale first, then the columns' ones.

@@ -31,7 +31,7 @@ namespace {
 // back in order.  So 128 x 15360 x 5120 with weights from memory takes 25 us, 64 rows 18.7, one 14.
 // ONCE: the weights are copied past the caches (see launch_split).
 template <int MB, int NB, int KW, int NS, int NW, bool ONCE>
-__global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearArgs a, int m_tiles, int n_tiles) {
+__global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearArgs a, QuantGrid grid) {
     constexpr int UNDER_WAY = (NS - 1) * 2 * MB + (NW - 1) * 2 * NB;   // copies of 1 KB behind a step's own
     static_assert(NS <= 2 && NW - NS <= 1 && NW >= NS && UNDER_WAY < 64, "counts of the waits");
     constexpr int OWN = (NS * MB + NW * NB) * 2048, RING = KW * OWN;
@@ -42,13 +42,16 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
     __shared__ __align__(16) float s_sx[16 * MB], s_sw[16 * NB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int mt, nt;
-    quant_tile_of(blockIdx.x, m_tiles, n_tiles * a.pieces, mt, nt);
+    // all arguments at once: loaded where they are used, they are several scalar round trips one behind the other
+    asm volatile("" ::"s"(a.x), "s"(a.x_scale), "s"(a.w), "s"(a.w_scale), "s"(a.x_ld), "s"(a.rows), "s"(a.cols), "s"(a.inner), "s"(a.chunks),
+                 "s"(a.pieces), "s"(grid.all), "s"(grid.band), "s"(grid.m_tiles));
+    quant_tile_of(grid, blockIdx.x, mt, nt);
     const int n_rb = (a.cols + QPACK_ROWS - 1) / QPACK_ROWS;
     const int k_last = (a.inner - 1) / 16 * 16;
     int step0 = 0, steps = (a.inner + 127) >> 7;   // (the packed weights may have one step of zeros more)
     if (a.pieces > 1) {
-        const int piece = nt / n_tiles, all = steps;
-        nt -= piece * n_tiles;
+        const int piece = fast_div(nt, grid.by_n), all = steps;
+        nt -= piece * grid.n_tiles;
         step0 = all * piece / a.pieces;
         steps = all * (piece + 1) / a.pieces - step0;
         a.y = static_cast<float*>(a.y) + static_cast<int64_t>(piece) * a.rows * a.y_ld;
@@ -155,12 +158,12 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
 constexpr int64_t CACHE_BYTES = int64_t{256} << 20;
 template <int MB, int NB, int KW, int NS, int NW>
 void launch_split(const QuantLinearArgs& a, int, hipStream_t st) {
-    const int m_tiles = (a.rows + 16 * MB - 1) / (16 * MB), n_tiles = (a.cols + 16 * NB - 1) / (16 * NB);
-    const bool once = a.cold ? m_tiles <= (MB <= 2 ? 2 : 1) : m_tiles == 1 && static_cast<int64_t>(a.cols) * a.inner >= CACHE_BYTES / 3;
+    const QuantGrid grid = quant_grid(a.rows, a.cols, a.pieces, 16 * MB, 16 * NB);
+    const bool once = a.cold ? grid.m_tiles <= (MB <= 2 ? 2 : 1) : grid.m_tiles == 1 && static_cast<int64_t>(a.cols) * a.inner >= CACHE_BYTES / 3;
     // weights that come past the caches, one step further ahead where the LDS holds it (63 x 27648 x 5120 30.0 -> 28.2 us)
     constexpr int ONCE_NW = NW == 1 && MB >= 4 && (MB + 2 * NB) * 2048 * KW < 156 * 1024 ? 2 : NW;
     hipLaunchKernelGGL((once ? cats_quant_linear_split<MB, NB, KW, NS, ONCE_NW, true> : cats_quant_linear_split<MB, NB, KW, NS, NW, false>),
-                       dim3(static_cast<unsigned>(m_tiles) * n_tiles * a.pieces), dim3(64 * KW), 0, st, a, m_tiles, n_tiles);
+                       dim3(grid.all), dim3(64 * KW), 0, st, a, grid);
 }
 
 // One wave moves one kilobyte: rows of 64 values in, an operand of the matrix instruction out.  vec: rows start at multiples of

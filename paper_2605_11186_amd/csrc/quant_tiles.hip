@@ -16,7 +16,7 @@ namespace {
 // Eight waves, two a SIMD: four waves of 128 x 128 each read less from LDS but wait alone (157 against 146 us), and the
 // 32x32x32 instruction, whose operands are runs of 256 bytes of the packed weights, is slower under load (153 against 144 us).
 template <int WM, int WN, int MB, int NB, int NS, int WS>
-__global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLinearArgs a, int m_tiles, int n_tiles) {
+__global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLinearArgs a, QuantGrid grid) {
     constexpr int WAVES = WM * WN, BM = 16 * WM * MB, BN = 16 * WN * NB;
     constexpr int COPIES = BM / 8 / WAVES;   // of a wave and step: 8 rows of 128 bytes each
     static_assert(4 % WS == 0, "places of W come round again after a pair of steps");
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
     static_assert(BM <= 64 * WAVES && BN <= 64 * WAVES, "one of each a thread");
     float sx_own, sw_own;
     auto enter = [&](int index) {
-        quant_tile_of(index, m_tiles, n_tiles, mt, nt);
+        quant_tile_of(grid, index, mt, nt);
         sx_own = a.x_scale[min(mt * BM + min(tid, BM - 1), a.rows - 1)];
         sw_own = a.w_scale[min(nt * BN + min(tid, BN - 1), a.cols - 1)];
         x0 = a.x + static_cast<int64_t>(mt) * BM * a.x_ld;
@@ -129,7 +129,6 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
         }
     };
     enter(blockIdx.x);
-    const int total = m_tiles * n_tiles;
     for (int index = blockIdx.x, parity = 0;; parity ^= 1) {
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES + NB) : "memory");
         if (tid < BM) s_sx[parity][tid] = sx_own;
@@ -155,7 +154,7 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
         const int t0 = mt * BM + wm * MB * 16, n0 = nt * BN + wn * NB * 16;
         const bool inside = nt * BN + BN <= a.cols;
         index += gridDim.x;
-        const bool more = index < total;
+        const bool more = index < grid.all;
         if (more) enter(index);
         // Four columns a lane are short runs of a row in bf16: a row block goes through LDS (each wave has its own place) and leaves
         // as eight columns a lane, whole lines of y.  With the scales read ahead: 4096 x 4096 x 256 16.6 -> 12.7 us.
@@ -197,9 +196,9 @@ __global__ __launch_bounds__(64 * WM * WN) void cats_quant_linear_tiles(QuantLin
 template <int WM, int WN, int MB, int NB, int NS, int WS>
 void launch_tiles(const QuantLinearArgs& a, int n_cus, hipStream_t st) {
     constexpr int BM = 16 * WM * MB, BN = 16 * WN * NB;
-    const int m_tiles = (a.rows + BM - 1) / BM, n_tiles = (a.cols + BN - 1) / BN;
-    hipLaunchKernelGGL((cats_quant_linear_tiles<WM, WN, MB, NB, NS, WS>), dim3(std::min(m_tiles * n_tiles, n_cus)),
-                       dim3(64 * WM * WN), 0, st, a, m_tiles, n_tiles);
+    const QuantGrid grid = quant_grid(a.rows, a.cols, 1, BM, BN);
+    hipLaunchKernelGGL((cats_quant_linear_tiles<WM, WN, MB, NB, NS, WS>), dim3(std::min(grid.all, n_cus)),
+                       dim3(64 * WM * WN), 0, st, a, grid);
 }
 
 }  // namespace
