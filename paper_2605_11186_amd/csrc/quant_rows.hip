@@ -5,8 +5,8 @@
 // One pass: a row is read once, held in the registers of the threads that share it (8 values a thread and piece)
 // until its maximum (for the norm its sum of squares first) is known, and written as bytes.  There is no matrix work and no more
 // than 20 instructions a value: the kernel is bound by memory with many rows and by its chain of loads, two reductions and
-// stores with few.  8192 x 5120 with a bf16 delta 85 us, 32000 x 4096 from bf16 68 us, SwiGLU of 4096 x 13824 53 us: 5.4 to 5.8
-// TB/s, where a large copy reaches 5.2; 63 rows of 4096 2.3 to 2.9 us, where an empty launch takes 1.6.
+// stores with few, every instruction of it counts.  8192 x 5120 with a bf16 delta 85 us, 32000 x 4096 from bf16 68 us, SwiGLU of 4096 x
+// 13824 52 us: 5.4 to 5.8 TB/s, where a large copy reaches 5.2; 63 rows of 4096 2.1 to 2.5 us, where an empty launch takes 1.6.
 #include <type_traits>
 
 #include "quant.hpp"
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float g = r0[j].get(e);
-                // (the hardware's reciprocal, 1 ulp: a division's ten instructions more made one row of 11008 take 4.4 us)
+                // (the hardware's reciprocal, 1 ulp: a division's ten instructions more cost half a microsecond in rows of 11008)
                 const float h = g * __builtin_amdgcn_rcpf(1.f + __expf(-g)) * r1[j].get(e);
                 v[j][e] = VEC || in[j][e] ? h : 0.f;
             }
@@ -336,8 +336,8 @@ void launch(const QuantRowsArgs& a, hipStream_t st) {
 }
 
 // Threads a row: few threads with a few pieces each wait for one another the least (two barriers a row) as long as a row's loads
-// are all under way at once.  Norm of 63 rows: 4096 columns 2.9 us with 256 threads, 3.6 with 1024; 11008 columns 4.9 with 512, 5.5
-// with 1024; 5120 columns 3.4 with 256 and three pieces, 3.7 with four.
+// are all under way at once.  Norm of 63 rows: 4096 columns 2.5 us with 256 threads, 2.6 with 512; 11008 columns 4.4 with 512 and
+// three pieces, 5.0 with 1024 and two; 5120 columns 2.9 with 256 and three pieces, 3.25 with 512 and two.
 template <int KIND, class T, class D, bool VEC>
 void by_size(const QuantRowsArgs& a, hipStream_t st) {
     const int pieces = (a.cols + 7) / 8;   // of 8 values
