@@ -356,7 +356,7 @@ int cats_rmsnorm_quantize(const float *x, int64_t x_ld, const void *delta, int32
                           const void *gain, float eps, int32_t rows, int32_t cols, float *x_out, int64_t x_out_ld,
                           int8_t *q, int64_t q_ld, float *scale, void *stream);
 
-/* SwiGLU and rows in 8 bits: gate_up [rows][2 cols] holds g | u, v = g / (1 + exp(-g)) * u. */
+/* SwiGLU and rows in 8 bits: gate_up [rows][2 cols] holds g | u, v = g / (1 + exp(-g)) * u (0 for finite g below -175). */
 int cats_swiglu_quantize(const void *gate_up, int32_t type, int64_t ld, int32_t rows, int32_t cols, int8_t *q, int64_t q_ld,
                          float *scale, void *stream);
 
