@@ -185,13 +185,19 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
     if (t >= a.rows) return;   // whole waves, and no barrier where a workgroup has several rows
     const int cols = a.cols;
     const T* src = static_cast<const T*>(a.src) + t * a.src_ld;
+    // 64 values a thread leave no registers for all that they are made of: that is read piece by piece.  (Read at once it is put by in
+    // memory, 340 to 650 bytes a thread: 63 rows of 20001 columns, norm with a float32 delta 70 us, 15 by piece; SwiGLU from float32 27 and 12.)
+    constexpr bool BY_PIECE = NC > 4 && (!VEC || sizeof(T) == 4) && (KIND == ROWS_SWIGLU || (KIND == ROWS_NORM && !VEC));
+    auto end_of_piece = [] {
+        if constexpr (BY_PIECE) __builtin_amdgcn_sched_barrier(0);
+    };
 
     Raw<T, VEC> r0[NC];
     float v[NC][8];
     bool in[NC][VEC ? 1 : 8];
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-        if constexpr (KIND != ROWS_MERGED) r0[j] = load8<T, TPR, VEC>(src, tid, j, cols);
+        if constexpr (KIND != ROWS_MERGED && !BY_PIECE) r0[j] = load8<T, TPR, VEC>(src, tid, j, cols);
 #pragma unroll
         for (int e = 0; e < (VEC ? 1 : 8); ++e) in[j][e] = place<TPR, VEC>(tid, j, e) < cols;
     }
@@ -209,9 +215,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
     } else if constexpr (KIND == ROWS_SWIGLU) {
         Raw<T, VEC> r1[NC];
 #pragma unroll
-        for (int j = 0; j < NC; ++j) r1[j] = load8<T, TPR, VEC>(src + cols, tid, j, cols);
+        for (int j = 0; j < NC; ++j)
+            if constexpr (!BY_PIECE) r1[j] = load8<T, TPR, VEC>(src + cols, tid, j, cols);
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
+            if constexpr (BY_PIECE) {
+                r0[j] = load8<T, TPR, VEC>(src, tid, j, cols);
+                r1[j] = load8<T, TPR, VEC>(src + cols, tid, j, cols);
+            }
             float lowest = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -227,6 +238,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[j][e] = VEC || in[j][e] ? v[j][e] : 0.f;
+            end_of_piece();
         }
     } else {
         Raw<bf16_t, VEC> rg[NC];
@@ -239,15 +251,24 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
             Raw<E, VEC> r1[PIECES][NC];
             const E* delta = static_cast<const E*>(a.delta) + t * a.delta_ld;
             float* out = a.x_out + t * a.x_out_ld;
+            auto load_delta = [&](int p, int j) {
+                r1[p][j] = load8<E, TPR, VEC>(delta + (PIECED ? min(p, a.delta_pieces - 1) * (a.rows * a.delta_ld) : 0), tid, j, cols);
+            };
+            if constexpr (!BY_PIECE) {
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p)
+                for (int p = 0; p < PIECES; ++p)
 #pragma unroll
-                for (int j = 0; j < NC; ++j)
-                    r1[p][j] = load8<E, TPR, VEC>(delta + (PIECED ? min(p, a.delta_pieces - 1) * (a.rows * a.delta_ld) : 0), tid, j, cols);
+                    for (int j = 0; j < NC; ++j) load_delta(p, j);
 #pragma unroll
-            for (int j = 0; j < NC; ++j) rg[j] = load8<bf16_t, TPR, VEC>(a.gain, tid, j, cols);
+                for (int j = 0; j < NC; ++j) rg[j] = load8<bf16_t, TPR, VEC>(a.gain, tid, j, cols);
+            }
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
+                if constexpr (BY_PIECE) {
+                    r0[j] = load8<T, TPR, VEC>(src, tid, j, cols);
+#pragma unroll
+                    for (int p = 0; p < PIECES; ++p) load_delta(p, j);
+                }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     float sum = r1[0][j].get(e);
@@ -266,13 +287,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
                     for (int e = 0; e < 8; ++e)
                         if (in[j][e]) out[place<TPR, VEC>(tid, j, e)] = v[j][e];
                 }
+                end_of_piece();
             }
         } else {
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                rg[j] = load8<bf16_t, TPR, VEC>(a.gain, tid, j, cols);
+                if constexpr (BY_PIECE)
+                    r0[j] = load8<T, TPR, VEC>(src, tid, j, cols);
+                else
+                    rg[j] = load8<bf16_t, TPR, VEC>(a.gain, tid, j, cols);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[j][e] = VEC || in[j][e] ? r0[j].get(e) : 0.f;
+                end_of_piece();
             }
         }
 #pragma unroll
@@ -292,9 +318,16 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void cats_quantize_rows_kern
         const float r = ss < INFINITY ? inverse_sqrt(ss * (1.f / static_cast<float>(cols)) + a.eps) : NAN;
         // (values that are not there are zeros, and NaN only where r or the last gains make the row's last values so, too)
 #pragma unroll
-        for (int j = 0; j < NC; ++j)
+        for (int j = 0; j < NC; ++j) {
+            if constexpr (BY_PIECE) {
+                int again = tid;   // (or else the places of all values are kept since the loads of x)
+                asm volatile("" : "+v"(again));
+                rg[j] = load8<bf16_t, TPR, VEC>(a.gain, again, j, cols);
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[j][e] = v[j][e] * r * rg[j].get(e);
+            end_of_piece();
+        }
     }
 
     // the largest |v|, as bits: ordered like the numbers, infinity above them and NaN above infinity
@@ -393,10 +426,12 @@ void by_size(const QuantRowsArgs& a, hipStream_t st) {
     if (pieces <= 256) return launch<KIND, T, D, 256, 1, VEC>(a, st);
     if (pieces <= 512) return launch<KIND, T, D, 256, 2, VEC>(a, st);
     if (pieces <= 768) return launch<KIND, T, D, 256, 3, VEC>(a, st);
-    if (pieces <= 1024) return launch<KIND, T, D, 512, 2, VEC>(a, st);
-    if (pieces <= 1536) return launch<KIND, T, D, 512, 3, VEC>(a, st);
-    if (pieces <= 2048) return launch<KIND, T, D, 512, 4, VEC>(a, st);
-    return launch<KIND, T, D, 1024, 8, VEC>(a, st);
+    if (pieces <= 1024 || std::is_same<D, pieces_t>::value) return launch<KIND, T, D, 512, 2, VEC>(a, st);
+    if constexpr (!std::is_same<D, pieces_t>::value) {   // (a delta of several pieces has the columns of a model's hidden rows, at most 8192)
+        if (pieces <= 1536) return launch<KIND, T, D, 512, 3, VEC>(a, st);
+        if (pieces <= 2048) return launch<KIND, T, D, 512, 4, VEC>(a, st);
+        return launch<KIND, T, D, 1024, 8, VEC>(a, st);
+    }
 }
 static_assert(CATS_QUANT_MAX_ROWS <= (1 << 21), "threads of a launch: fewer than 2^32");
 static_assert(CATS_QUANT_MAX_COLS == 1024 * 8 * 8, "the longest row fills the largest workgroup's registers");
