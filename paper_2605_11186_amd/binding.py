@@ -332,13 +332,31 @@ def cats_packed_matrix_bytes(rows: int, cols: int) -> int:
     return int(library().cats_packed_matrix_bytes(int(rows), int(cols)))
 
 
+def _packed_on(stream, src, dst, pack):
+    """dst from src by pack(stream handle) on the stream, behind what torch's current stream has queued, whose tensors they are,
+    and ahead of what it queues next (so that src may be dropped and dst be used there)."""
+    import torch
+    current = torch.cuda.current_stream(src.device)
+    if stream is None or stream == 0:
+        target = torch.cuda.default_stream(src.device)
+    else:
+        target = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=src.device)
+    apart = target.cuda_stream != current.cuda_stream
+    if apart:
+        target.wait_stream(current)
+    _check(pack(target.cuda_stream))
+    if apart:
+        current.wait_stream(target)
+    return dst
+
+
 def cats_pack_matrix(src, stream=None):
-    """Packed copy of a row-major bf16 [rows][cols] device tensor (new device tensor, bf16)."""
+    """Packed copy of a row-major bf16 [rows][cols] device tensor (new device tensor, bf16).  Ordered with torch's current stream,
+    whichever stream it runs on."""
     import torch
     rows, cols = src.shape
     dst = torch.empty(cats_packed_matrix_bytes(rows, cols) // 2, dtype=torch.bfloat16, device=src.device)
-    _check(library().cats_pack_matrix(_dp(src), _dp(dst), int(rows), int(cols), _stream(stream)))
-    return dst
+    return _packed_on(stream, src, dst, lambda st: library().cats_pack_matrix(src.data_ptr(), dst.data_ptr(), rows, cols, st))
 
 
 MATRIX_FIELDS = ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down")
@@ -489,7 +507,8 @@ def cats_packed_quantized_bytes(rows: int, cols: int) -> int:
 
 
 def cats_pack_quantized_matrix(src, stream=None):
-    """Packed copy of int8 weights [out][in] (new device tensor, int8)."""
+    """Packed copy of int8 weights [out][in] (new device tensor, int8).  Ordered with torch's current stream, whichever stream it
+    runs on."""
     import torch
     if _f32 is None:
         _load_types()
@@ -500,8 +519,9 @@ def cats_pack_quantized_matrix(src, stream=None):
     dst = torch.empty(cats_packed_quantized_bytes(rows, cols), dtype=torch.int8, device=src.device)
     if rows == 1:
         ld = _single_row(cols)
-    _check(library().cats_pack_quantized_matrix(src.data_ptr(), ld, rows, cols, dst.data_ptr(), _stream_on(dev, stream)))
-    return dst
+    _stream_on(dev, stream)
+    return _packed_on(stream, src, dst,
+                      lambda st: library().cats_pack_quantized_matrix(src.data_ptr(), ld, rows, cols, dst.data_ptr(), st))
 
 
 def cats_quantized_linear(x, x_scale, w_packed, w_scale, out, stream=None):
