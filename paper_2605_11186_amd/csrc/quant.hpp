@@ -5,8 +5,8 @@
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-// CATS_EHIP; cats_strerror then gives the text of e.
-int hip_fail(hipError_t e);
+// CATS_EHIP; cats_strerror then gives the text of e.  Hidden: a name like any other's, which another library must not take the place of.
+__attribute__((visibility("hidden"))) int hip_fail(hipError_t e);
 // The status behind a launch.
 inline int launch_status() {
     const hipError_t e = hipGetLastError();
