@@ -541,7 +541,7 @@ def cats_quantized_linear(x, x_scale, w_packed, w_scale, out, stream=None):
                          w_scale=(w_scale, _f32, (cols,)), out=(out, (_f32, _bf16), (rows, cols)))
     if rows == 1:
         ld, y_ld = _single_row(inner), _single_row(cols)
-    if inner % 16 and x.untyped_storage().nbytes() < x.storage_offset() + (rows - 1) * ld + (inner + 15) // 16 * 16:
+    if rows and inner % 16 and x.untyped_storage().nbytes() < x.storage_offset() + (rows - 1) * ld + (inner + 15) // 16 * 16:
         raise CatsError(CATS_EINVAL, "x: its last row must be readable up to a multiple of 16 bytes")
     if rows:
         _check(library().cats_quantized_linear(x.data_ptr(), ld, x_scale.data_ptr(), w_packed.data_ptr(), w_scale.data_ptr(),
