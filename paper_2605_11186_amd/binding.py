@@ -418,6 +418,11 @@ def _refuse_operands(device, **operands):
     raise CatsError(CATS_EINVAL, f"tensors on device {device}, which is not the current GPU")
 
 
+def _refuse_dimensions(**operands):
+    text = ", ".join(f"{name} {list(t.shape)}" for name, t in operands.items() if t is not None)
+    raise CatsError(CATS_EINVAL, f"tensors of rows and columns expected, got {text}") from None
+
+
 def _stream_on(device, stream):
     """A stream's handle (a torch stream's or the number itself); a torch stream has to belong to the tensors' device."""
     if stream is None:
@@ -436,9 +441,12 @@ def cats_quantize_rows(src, q_out, scale_out, stream=None):
     """Rows of src (float32 or bfloat16 [rows][cols]) as int8 with one float32 scale each."""
     if _f32 is None:
         _load_types()
-    rows, cols = shape = src.shape
+    try:
+        rows, cols = shape = src.shape
+        (ld, step), (q_ld, q_step) = src.stride(), q_out.stride()
+    except ValueError:
+        _refuse_dimensions(src=src, q_out=q_out)
     dev, code = src.get_device(), _code_of.get(src.dtype)
-    (ld, step), (q_ld, q_step) = src.stride(), q_out.stride()
     if (code is None or q_out.dtype is not _i8 or scale_out.dtype is not _f32 or q_out.shape != shape or scale_out.shape != (rows,) or
             (cols > 1 and (step != 1 or q_step != 1)) or not scale_out.is_contiguous() or q_out.get_device() != dev or
             scale_out.get_device() != dev or dev < 0 or dev != _current_device()):
@@ -456,13 +464,17 @@ def cats_rmsnorm_quantize(x, gain, eps: float, q_out, scale_out, delta=None, x_o
     goes to x_out, or back to x if none is given."""
     if _f32 is None:
         _load_types()
-    rows, cols = shape = x.shape
     dev = x.get_device()
-    (ld, step), (q_ld, q_step) = x.stride(), q_out.stride()
     d_ptr, d_code, d_ld, o_ptr, o_ld, ok = None, 0, 0, None, 0, True
+    try:
+        rows, cols = shape = x.shape
+        (ld, step), (q_ld, q_step) = x.stride(), q_out.stride()
+        if delta is not None:
+            out = x if x_out is None else x_out
+            (d_ld, d_step), (o_ld, o_step) = delta.stride(), out.stride()
+    except ValueError:
+        _refuse_dimensions(x=x, q_out=q_out, delta=delta, x_out=x_out)
     if delta is not None:
-        out = x if x_out is None else x_out
-        (d_ld, d_step), (o_ld, o_step) = delta.stride(), out.stride()
         d_code, d_ptr, o_ptr = _code_of.get(delta.dtype), delta.data_ptr(), out.data_ptr()
         ok = (d_code is not None and delta.shape == shape and out.shape == shape and out.dtype is _f32 and
               (cols == 1 or d_step == o_step == 1) and delta.get_device() == dev and out.get_device() == dev)
@@ -487,9 +499,12 @@ def cats_swiglu_quantize(gate_up, q_out, scale_out, stream=None):
     """silu(gate) * up of gate_up (float32 or bfloat16 [rows][2 cols], gate | up) as int8 rows with scales."""
     if _f32 is None:
         _load_types()
-    rows, cols = q_out.shape
+    try:
+        rows, cols = q_out.shape
+        (ld, step), (q_ld, q_step) = gate_up.stride(), q_out.stride()
+    except ValueError:
+        _refuse_dimensions(gate_up=gate_up, q_out=q_out)
     dev, code = gate_up.get_device(), _code_of.get(gate_up.dtype)
-    (ld, step), (q_ld, q_step) = gate_up.stride(), q_out.stride()
     if (code is None or q_out.dtype is not _i8 or scale_out.dtype is not _f32 or gate_up.shape != (rows, 2 * cols) or
             scale_out.shape != (rows,) or step != 1 or (cols > 1 and q_step != 1) or not scale_out.is_contiguous() or
             q_out.get_device() != dev or scale_out.get_device() != dev or dev < 0 or dev != _current_device()):
@@ -512,8 +527,11 @@ def cats_pack_quantized_matrix(src, stream=None):
     import torch
     if _f32 is None:
         _load_types()
-    rows, cols = src.shape
-    dev, (ld, step) = src.get_device(), src.stride()
+    try:
+        (rows, cols), (ld, step) = src.shape, src.stride()
+    except ValueError:
+        _refuse_dimensions(src=src)
+    dev = src.get_device()
     if src.dtype is not _i8 or (cols > 1 and step != 1) or dev < 0 or dev != _current_device():
         _refuse_operands(dev, src=(src, _i8, (rows, cols)))
     dst = torch.empty(cats_packed_quantized_bytes(rows, cols), dtype=torch.int8, device=src.device)
@@ -528,9 +546,12 @@ def cats_quantized_linear(x, x_scale, w_packed, w_scale, out, stream=None):
     """out [rows][cols] (float32 or bfloat16) = (x . W) * x_scale * w_scale for int8 x [rows][inner] and packed int8 W [cols][inner]."""
     if _f32 is None:
         _load_types()
-    (rows, inner), (out_rows, cols) = x.shape, out.shape
+    try:
+        (rows, inner), (out_rows, cols) = x.shape, out.shape
+        (ld, step), (y_ld, y_step) = x.stride(), out.stride()
+    except ValueError:
+        _refuse_dimensions(x=x, out=out)
     dev, code = x.get_device(), _code_of.get(out.dtype)
-    (ld, step), (y_ld, y_step) = x.stride(), out.stride()
     packed = (cols + 15) // 16 * ((inner + 255) // 256) * 4096
     if (code is None or x.dtype is not _i8 or w_packed.dtype is not _i8 or x_scale.dtype is not _f32 or w_scale.dtype is not _f32 or
             out_rows != rows or x_scale.shape != (rows,) or w_scale.shape != (cols,) or w_packed.shape != (packed,) or
