@@ -41,12 +41,17 @@ inline int quant_tile_choice(int rows, int cols, int n_cus, int pieces = 1, int6
 // Many rows: tiles that fill a round of compute units and a few more leave the chip idle for most of the next one.  Then the first
 // columns, whole rounds of one of the four largest tiles, are one launch and the others another, in the tiles that suit them best.
 // 700 x 22016 x 4096 90 us as 258 tiles of 256 x 256, 66.5 as 255 of them and 256 columns in tiles of 32 x 32; 1500 x 12288 x 4096 88 and
-// 73.  The tiles of 192 columns fill the chip where those of 256 do not: 256 x 22016 x 4096 43.6 -> 37.0, 300 x 15360 x 5120 43.5 -> 35.5.
+// 73.  What the second launch costs, a start and, at any inner length, some operands that nothing hides, decides where little is
+// gained: of 127 sizes with two launches by the tiles and the start alone the 40 that go out in one took 7 % more to 6 % less time in two, 1 %
+// more on average (1500 x 4096 x 11008 68 us, 71 in two; 300 x 22016 x 4096 44.5 and 46), the other 87 take 13 % more to 27 % less, 6 % less
+// on average; what loses still is of short inner lengths (1200 x 15360 x 1024 27.6, 31 in two).
+// The tiles of 192 columns fill the chip where those of 256 do not: 256 x 22016 x 4096 43.6 -> 37.0, 300 x 15360 x 5120 43.5 -> 35.5.
 struct QuantPlan {
     int tile, cols;     // of the first launch; cols: all of them, or the first ones, a multiple of 64
     int rest_tile;      // of the second, if there is one
 };
 constexpr int LAUNCH_COST = 40;   // of the second launch, at inner = 4096
+constexpr int SECOND_COST = 50;   // and at any inner length
 inline QuantPlan quant_plan(int rows, int cols, int inner, int n_cus) {
     int64_t least;
     QuantPlan best{quant_tile_choice(rows, cols, n_cus, 1, &least), cols, 0};
@@ -60,7 +65,7 @@ inline QuantPlan quant_plan(int rows, int cols, int inner, int n_cus) {
         const int main_cols = static_cast<int>(n_main) * c.bn;
         int64_t rest;
         const int rest_tile = quant_tile_choice(rows, cols - main_cols, n_cus, 1, &rest);
-        const int64_t cost = ((m_tiles * n_main + n_cus - 1) / n_cus * c.cost + rest) * inner + int64_t{LAUNCH_COST} * 4096;
+        const int64_t cost = ((m_tiles * n_main + n_cus - 1) / n_cus * c.cost + rest + SECOND_COST) * inner + int64_t{LAUNCH_COST} * 4096;
         if (cost < least) {
             least = cost;
             best = {i, main_cols, rest_tile};
