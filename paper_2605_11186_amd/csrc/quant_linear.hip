@@ -151,10 +151,16 @@ __global__ __launch_bounds__(64 * KW) void cats_quant_linear_split(QuantLinearAr
 }
 
 // Weights that will hardly be found in the 256 MB cache in front of the memory by the next call are copied past the caches, which then
-// keep other things: a matrix of a third of that size or more that one row tile reads, and whatever the caller calls cold, also
-// for two tiles of up to 32 rows (which read it side by side; larger pairs lose by it).  64 x 27648 x 5120 33 -> 28.5 us; 63 x 22016 x 4096 with twelve matrices in turn
-// 22.8 -> 20.1, one row 17.2 -> 15.7, with three (270 MB) 19.9 -> 19.6; 63 x 4096 x 11008, forty in turn, 17.3 -> 15.5.  Smaller
-// ones may be of a model that the cache holds: three of 4096 x 11008 in turn take 8.4 us with one row, past the caches 9.8.
+// keep other things: a matrix that one row tile reads and that takes a third of that size or more, so that three like it do not stay
+// there, and whatever the caller calls cold, also for two tiles of up to 32 rows (which read it side by side; larger pairs lose by
+// it).  The size is all that a call knows of its weights' whereabouts; us through the caches -> past them, matrices in turn that
+// come from memory | one or two that the cache holds:
+//   79 MB (15360 x 5120), below the border: one row 15.6 -> 14.2 | 13.1 -> 12.4 to 13.3, 63 rows 21.2 -> 18.3 | 16.1 -> 16.3 to 17.3,
+//     128 rows 28.0 -> 24.5 | 19.7 -> 22.7 to 23.6; three of them, 236 MB, 63 rows 16.1 -> 17.6
+//   90 MB (22016 x 4096): one row 17.3 -> 16.0 | 14.7 -> 14.0 to 14.6, 63 rows 22.6 -> 19.8 | 18.5 -> 17.8 to 18.8, 128 rows
+//     28.4 -> 25.2 | 22.4 -> 23.3 to 24.1; three of them, 271 MB, even: 63 rows 19.1 -> 19.3
+//   205 MB (40000 x 5120): one row 37.3 -> 33.2 | 29.4 -> 31.4, 63 rows 50.7 -> 45.5 | 37.8 -> 43.0
+// Smaller ones gain less from memory and lose more from the cache (34 MB, 8192 x 4096, one row 7.7 -> 7.2 | 4.1 -> 5.9).
 constexpr int64_t CACHE_BYTES = int64_t{256} << 20;
 template <int MB, int NB, int KW, int NS, int NW>
 void launch_split(const QuantLinearArgs& a, int, hipStream_t st) {

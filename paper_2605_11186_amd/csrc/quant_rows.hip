@@ -6,7 +6,7 @@
 // until its maximum (for the norm its sum of squares first) is known, and written as bytes.  There is no matrix work and no more
 // than 20 instructions a value: the kernel is bound by memory with many rows and by its chain of loads, two reductions and
 // stores with few, every instruction of it counts.  8192 x 5120 with a bf16 delta 85 us, 32000 x 4096 from bf16 68 us, SwiGLU of 4096 x
-// 13824 52 us: 5.4 to 5.8 TB/s, where a large copy reaches 5.2; 63 rows of 4096 2.1 to 2.5 us, where an empty launch takes 1.6.
+// 13824 52 us: 5.4 to 5.8 TB/s, where a large copy reaches 5.2; 63 rows of 4096 2.0 to 2.5 us, where an empty launch takes 1.6.
 #include <type_traits>
 
 #include "quant.hpp"
