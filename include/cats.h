@@ -389,7 +389,8 @@ typedef struct {
 /* Layers [layer_begin, layer_end) of `layers` (HOST array indexed by layer) over all T tree nodes, as cats_verify_layer runs
  * them, with every product's input in 8 bits: the operators above, and rotation, cache append and tree attention as in
  * the other calls (the cache is bf16, queries and the call's own rows carry about 16 mantissa bits).  The attention output is rounded to bf16 before
- * it is quantised, the other products' outputs stay float32.  hidden: float32 [T][hidden], 16-byte aligned, in/out.  kv: HOST array
+ * it is quantised, the other products' outputs stay float32.  A row that is not finite spreads as it does in the other calls: a node's keys and
+ * values that are not numbers make the attention of all nodes not a number.  hidden: float32 [T][hidden], 16-byte aligned, in/out.  kv: HOST array
  * indexed by layer.  The context's packed_weights plays no part, and cats_profile_gemm does not count these products.
  * A whole step: cats_set_tree, embedding rows in hidden, this call, cats_lm_head_argmax, cats_accept_and_compact.
  * CATS_EINVAL: a bad layer range, a NULL or misaligned pointer in a layer of the range (weights 16 bytes, scales 4, gains 2), hidden NULL or
