@@ -10,6 +10,7 @@ import pytest
 import paper_2605_11186_amd as cats
 
 READELF = Path("/opt/rocm/llvm/bin/llvm-readelf")
+pytestmark = pytest.mark.skipif(not READELF.exists(), reason="ROCm's readelf is not there")
 MAGIC = b"__CLANG_OFFLOAD_BUNDLE__"
 
 
